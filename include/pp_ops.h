@@ -1,4 +1,4 @@
-/* pp_ops.h -- op-level entry points of the same library: the dense contractions of the local step, callable
+/* pp_ops.h -- op-level entry points of the same library: the dense contractions of the local step and the losses of its output head, callable
  * on their own so that each kernel can be checked against a plain definition and timed against its roofline.
  * All pointers are device pointers owned by the caller; all calls only enqueue work on `hip_stream`.
  * dtype: PP_F32 or PP_BF16 storage (see pp.h).  Return PP_OK or a negative PP_E* code (pp_last_error()).
@@ -63,6 +63,42 @@ int pp_op_attention_fwd(void* hip_stream, int dtype, const void* qkv_dev, void* 
  * D_dev: float [B*h*S], receives the row sums of dO * O.  scratch_dev: not used, may be NULL. */
 int pp_op_attention_bwd(void* hip_stream, int dtype, const void* qkv_dev, const void* o_dev, const float* lse_dev, const void* dO_dev,
                         void* dqkv_dev, float* D_dev, void* scratch_dev, int B, int S, int h, int dh, int path);
+
+/* ---- Losses of the output head over a large vocabulary, without the logits being kept.
+ *
+ * z = X W^T for hidden states X [n x d] and head weights W [vocab x d] (row-major, ldx and ldw elements apart); z exists a piece of rows
+ * at a time, in the workspace, and never as a whole.  One call forms the losses and, where asked for, the gradients
+ *   dX = dz W [n x d]   and   dW = dz^T X for the rows [dw_lo, dw_hi) of W
+ * of   loss = sum_t w_t l_t,   w_t = row_weight[t], or 1 / (number of rows that are not left out) where row_weight is NULL (the mean, as in pp_local_step).
+ *   pp_op_head_ce       l_t = lse(z_t) - z_t[target]; a row whose target is outside [0, vocab) is left out.
+ *   pp_op_head_distill  l_t = (1 - share) CE_t + share temperature^2 KL(q_t || softmax(z_t / temperature)) with CE_t as above and
+ *                       q_t = softmax(logits_t / temperature) over the `top` entries (id, logit) that the teacher lists for the row.  An id outside [0, vocab) or a logit of
+ *                       -inf is no entry, whatever its other half holds; equal ids add up.  A row without entries has no KL term, a row without target no CE term, a row without
+ *                       either (terms with a share of 0 do not count) is left out.
+ * A row of weight 0 is left out too.  Rows that are left out have row_loss = row_lse = 0 and a dX row of zeros, and neither their values nor infinities or NaN among them reach
+ * anything else.  n == 0 gives loss 0 and dW = 0.
+ * Sums, exponentials and losses are fp32.  With bf16 storage the exponentials of a row are rounded to bf16 (at most 2^-8 relative) on their way into the gradients'
+ * products, as are the rows of X scaled by w_t over the softmax's sum; dX is rounded once from fp32 sums.  Results do not depend on the run. */
+#define PP_HEAD_TOP_MAX 128
+typedef struct {
+  const void *x, *w;               /* storage type dtype */
+  const float* row_weight;         /* [n] or NULL */
+  float* loss;                     /* [1] or NULL */
+  float *row_loss, *row_lse;       /* [n] or NULL: l_t; log-sum-exp of z_t / temperature (pp_op_head_ce: of z_t) */
+  void *dx, *dw;                   /* dx [n x d], storage type, or NULL; dw [(dw_hi - dw_lo) x d], or NULL if dw_lo == dw_hi.  Neither may overlap an input. */
+  int32_t ldx, ldw, lddx, lddw;    /* elements from row to row, >= d (lddx, lddw: where dx, dw are given) */
+  int32_t dtype, n, vocab, d;      /* PP_F32 or PP_BF16; n <= 2^24, vocab <= 2^20, d <= 2^14 */
+  int32_t dw_lo, dw_hi;            /* 0 <= dw_lo <= dw_hi <= vocab; row 0 of dw is row dw_lo of W */
+  int32_t dw_f32;                  /* 0: dw in storage type; 1: dw float; 2: dw float, and the gradient is added to what it holds */
+  int32_t piece;                   /* rows of a piece, rounded up to a multiple of 64; 0: as many as keep a piece's buffer within 512 MiB */
+} pp_head;
+/* Workspace of a call with these sizes, options and operand alignment (top: entries per row, 0 for pp_op_head_ce); 0 and an error text on invalid arguments. */
+size_t pp_op_head_bytes(const pp_head* head, int32_t top);
+/* targets_dev: int32 [n].  ws_dev: 256-byte aligned, ws_bytes >= pp_op_head_bytes; the content does not matter and is not kept.  Calls that overlap need a workspace each. */
+int pp_op_head_ce(void* hip_stream, const pp_head* head, const int32_t* targets_dev, void* ws_dev, size_t ws_bytes);
+/* ids_dev: int32 [n x top], logits_dev: float [n x top], 1 <= top <= PP_HEAD_TOP_MAX; temperature in [2^-6, 2^6]; share in [0, 1]; targets_dev may be NULL if share == 1. */
+int pp_op_head_distill(void* hip_stream, const pp_head* head, const int32_t* ids_dev, const float* logits_dev, int32_t top, float temperature, float share,
+                       const int32_t* targets_dev, void* ws_dev, size_t ws_bytes);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,8 @@ What it computes (paper: "Partial Parameter Updates", Algorithm 1 and Section 2.
                          weight decay either).
   * outer_step():        Alg. 1's delta, count normalisation and OuterOpt (Nesterov-momentum SGD,
                          Experimental Setup) for the node's own trainable subset.
+  * head_loss():         the losses of the output head alone (cross entropy, distillation from a teacher's
+                         top logits) with their gradients.
   * flops_forward / flops_backward_ffn_slice / flops_backward_all: closed forms for the matmul
                          FLOPs the step executes;  paper_flops: the paper's own closed forms.
 
@@ -39,6 +41,7 @@ library autograd + library AdamW with decayed / undecayed parameter groups; its 
 against the library's bf16 cast; closed forms (rotary, AdamW step 1, Nesterov step 1, loss ~ ln V at init);
 invariants (causality, slice additivity of the FFN, masked == slice of full, frozen unchanged);
 the detach ablation against library autograd with the dropped units' activations detached;
+head_loss against library autograd and central differences (tests/test_head_loss.py);
 FLOP counter == closed form; the paper's FLOP formulas reproduce its "15% fewer FLOPs" and its
 rho=1 identity; Table 1's trainable-parameter column.
 Parity unpinned: Table 1 perplexities / memory GB and the 0.44 s step time (need the paper's
@@ -568,3 +571,47 @@ def outer_step(theta_g, theta_l, others_sum, momentum_buf, lr, mu, m_count, nest
     b = mu * momentum_buf + delta
     upd = delta + mu * b if nesterov else b
     return theta_g - lr * upd, b, delta
+
+
+def head_loss(x, w, targets, row_weight=None, ids=None, logits=None, tau=1.0, share=1.0):
+    """Losses of the output head from their definition, and their gradients: cross entropy where ids is None, else (1 - share) CE + share tau^2 KL(teacher || student) with the
+    teacher's softmax over its listed entries only.  Returns loss, row_loss, row_lse, z, dz, dx, dw (all rows of w) and live (rows that are not left out)."""
+    x, w = np.asarray(x, F64), np.asarray(w, F64)
+    n, vocab = x.shape[0], w.shape[0]
+    if ids is None:
+        tau, share = 1.0, 0.0
+    hard = np.zeros(n, bool) if targets is None or share == 1.0 else (targets >= 0) & (targets < vocab)
+    soft = np.zeros(n, bool)
+    if ids is not None and share > 0:
+        there = (ids >= 0) & (ids < vocab)
+        there &= np.where(there, logits, -np.inf) != -np.inf
+        soft = there.any(axis=1)
+    if row_weight is not None:
+        hard, soft = hard & (row_weight != 0), soft & (row_weight != 0)
+    live = hard | soft
+    g = np.asarray(row_weight, F64) if row_weight is not None else np.full(n, 1.0 / max(1, int(live.sum())))
+    z, dz = np.zeros((n, vocab)), np.zeros((n, vocab))
+    row_loss, row_lse = np.zeros(n), np.zeros(n)
+
+    def softmax(v):
+        m = v.max()
+        e = np.exp(v - m)
+        return e / e.sum(), m + np.log(e.sum())
+
+    for t in np.nonzero(live)[0]:
+        z[t] = w @ x[t]
+        pt, row_lse[t] = softmax(z[t] / tau)
+        if hard[t]:
+            p, lse = softmax(z[t])
+            row_loss[t] += (1.0 - share) * (lse - z[t, targets[t]])
+            dz[t] += (1.0 - share) * p
+            dz[t, targets[t]] -= 1.0 - share
+        if soft[t]:
+            at = ids[t, there[t]]
+            q, _ = softmax(np.asarray(logits[t, there[t]], F64) / tau)
+            row_loss[t] += share * tau ** 2 * np.sum(np.where(q > 0, q * (np.log(np.where(q > 0, q, 1.0)) - z[t, at] / tau + row_lse[t]), 0.0))
+            dz[t] += share * tau * pt
+            np.subtract.at(dz[t], at, share * tau * q)
+        dz[t] *= g[t]
+    x0 = np.where(live[:, None], x, 0.0)
+    return dict(loss=float(np.sum(np.where(live, g, 0.0) * row_loss)), row_loss=row_loss, row_lse=row_lse, z=z, dz=dz, dx=dz @ w, dw=dz.T @ x0, live=live)

@@ -13,10 +13,12 @@ import numpy as np
 
 PP_F32, PP_BF16 = 0, 1
 PP_STATIC_SCRATCH_FLOATS = 4 << 20          # include/pp_ops.h
+PP_HEAD_TOP_MAX = 128                       # include/pp_ops.h
 PP_BYTES_PARAMS, PP_BYTES_STATE, PP_BYTES_WORKSPACE, PP_BYTES_SHADOW, PP_BYTES_ACTIVATIONS = range(5)
 EXPORTS = ["pp_query_bytes", "pp_init_model", "pp_set_tensor", "pp_get_tensor", "pp_set_trainable_mask", "pp_local_step",
            "pp_set_jacobian_slices", "pp_outer_delta", "pp_outer_delta_group", "pp_synth_delta_sum", "pp_get_counters", "pp_get_launch_counts", "pp_get_gemm_timing", "pp_set_option", "pp_last_error", "pp_free",
-           "pp_op_gemm_nt", "pp_op_gemm_tn", "pp_op_gemm_nt_splitk_static", "pp_op_attention_fwd", "pp_op_attention_bwd"]
+           "pp_op_gemm_nt", "pp_op_gemm_tn", "pp_op_gemm_nt_splitk_static", "pp_op_attention_fwd", "pp_op_attention_bwd",
+           "pp_op_head_bytes", "pp_op_head_ce", "pp_op_head_distill"]
 
 
 class PPError(RuntimeError):
@@ -39,6 +41,11 @@ class PPAdamW(C.Structure):
 
 class PPOuter(C.Structure):
     _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("nesterov", C.c_int32), ("m_count", C.c_float)]
+
+
+class PPHead(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "w", "row_weight", "loss", "row_loss", "row_lse", "dx", "dw")] + \
+               [(n, C.c_int32) for n in ("ldx", "ldw", "lddx", "lddw", "dtype", "n", "vocab", "d", "dw_lo", "dw_hi", "dw_f32", "piece")]
 
 
 def lib_path() -> str:
@@ -102,6 +109,12 @@ def load_library():
     lib.pp_op_attention_fwd.argtypes = [vp, C.c_int, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]
     lib.pp_op_attention_bwd.restype = C.c_int
     lib.pp_op_attention_bwd.argtypes = [vp, C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int]
+    lib.pp_op_head_bytes.restype = sz
+    lib.pp_op_head_bytes.argtypes = [C.POINTER(PPHead), i32]
+    lib.pp_op_head_ce.restype = C.c_int
+    lib.pp_op_head_ce.argtypes = [vp, C.POINTER(PPHead), vp, vp, sz]
+    lib.pp_op_head_distill.restype = C.c_int
+    lib.pp_op_head_distill.argtypes = [vp, C.POINTER(PPHead), vp, vp, i32, C.c_float, C.c_float, vp, vp, sz]
     _lib = lib
     return lib
 
@@ -219,6 +232,48 @@ def pp_op_attention_fwd(stream: int, dtype: int, qkv_ptr, o_ptr, lse_ptr, scratc
 def pp_op_attention_bwd(stream: int, dtype: int, qkv_ptr, o_ptr, lse_ptr, dO_ptr, dqkv_ptr, D_ptr, scratch_ptr, B, S, h, dh, path=0):
     _check(load_library().pp_op_attention_bwd(stream, dtype, qkv_ptr, o_ptr, lse_ptr, dO_ptr, dqkv_ptr, D_ptr, scratch_ptr, B, S, h, dh, path),
            "pp_op_attention_bwd")
+
+
+def pp_op_head_bytes(head: PPHead, top: int = 0) -> int:
+    n = load_library().pp_op_head_bytes(C.byref(head), top)
+    if n == 0:
+        raise PPError("pp_op_head_bytes failed: " + pp_last_error())
+    return n
+
+
+def pp_op_head_ce(stream: int, head: PPHead, targets_ptr, ws_ptr, ws_bytes: int):
+    _check(load_library().pp_op_head_ce(stream, C.byref(head), targets_ptr, ws_ptr, ws_bytes), "pp_op_head_ce")
+
+
+def pp_op_head_distill(stream: int, head: PPHead, ids_ptr, logits_ptr, top: int, temperature: float, share: float, targets_ptr, ws_ptr, ws_bytes: int):
+    _check(load_library().pp_op_head_distill(stream, C.byref(head), ids_ptr, logits_ptr, top, temperature, share, targets_ptr, ws_ptr, ws_bytes), "pp_op_head_distill")
+
+
+def make_head(x, w, *, row_weight=None, loss=None, row_loss=None, row_lse=None, dx=None, dw=None, dw_lo=0, dw_hi=None, dw_add=False, piece=0) -> PPHead:
+    """The pp_head of torch tensors (include/pp_ops.h): x [n, d], w [vocab, d], dx [n, d], dw [dw_hi - dw_lo, d] with columns next to each other, the others
+    contiguous float.  dw is of w's type or float32; dw_add adds to a float32 dw.  The tensors are kept alive by the returned object."""
+    import torch
+    n, d, vocab, f32 = x.shape[0], x.shape[1], w.shape[0], torch.float32
+    if x.dtype not in (f32, torch.bfloat16) or w.dtype != x.dtype:
+        raise PPError("make_head: x and w must both be float32 or both bfloat16")
+    if dw_hi is None:
+        dw_hi = dw_lo + (dw.shape[0] if dw is not None else 0)
+    for name, t, shape, types in (("x", x, (n, d), (x.dtype,)), ("w", w, (vocab, d), (x.dtype,)), ("dx", dx, (n, d), (x.dtype,)), ("dw", dw, (dw_hi - dw_lo, d), (x.dtype, f32)),
+                                  ("row_weight", row_weight, (n,), (f32,)), ("loss", loss, (1,), (f32,)), ("row_loss", row_loss, (n,), (f32,)), ("row_lse", row_lse, (n,), (f32,))):
+        if t is None:
+            continue
+        if tuple(t.shape) != shape or t.dtype not in types or t.device != x.device:
+            raise PPError(f"make_head: {name} must be {shape} of {' or '.join(str(k) for k in types)} on {x.device}")
+        if t.numel() and t.stride(-1) != 1 or t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < d:
+            raise PPError(f"make_head: {name}: elements of a row must lie next to each other, rows one after the other")
+    if dw_add and (dw is None or dw.dtype != f32):
+        raise PPError("make_head: dw_add needs a float32 dw")
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    ld = lambda t: d if t is None or t.shape[0] < 2 else t.stride(0)  # noqa: E731
+    h = PPHead(ptr(x), ptr(w), ptr(row_weight), ptr(loss), ptr(row_loss), ptr(row_lse), ptr(dx), ptr(dw), ld(x), ld(w), ld(dx), ld(dw), PP_F32 if x.dtype == f32 else PP_BF16, n, vocab, d,
+               dw_lo, dw_hi, 0 if dw is None else 2 if dw_add else 1 if dw.dtype == f32 else 0, piece)
+    h.tensors = (x, w, row_weight, loss, row_loss, row_lse, dx, dw)
+    return h
 
 
 # --------------------------------------------------------------------------------------------- convenience holder

@@ -1045,3 +1045,62 @@ extern "C" int pp_op_attention_bwd(void* hip_stream, int dtype, const void* qkv,
   if (e != hipSuccess) return fail(PP_EHIP, std::string("pp_op_attention_bwd: ") + hipGetErrorString(e));
   return PP_OK;
 }
+
+// ---- losses of the output head
+static int check_head(const pp_head* h, int top, HeadArgs* a) {
+  if (!h) return fail(PP_EINVAL, "head: NULL");
+  if (h->dtype != PP_F32 && h->dtype != PP_BF16) return fail(PP_EINVAL, "head: dtype must be PP_F32 or PP_BF16");
+  if (h->n < 0 || h->n > 1 << 24) return fail(PP_EINVAL, "head: n outside [0, 2^24]");
+  if (h->vocab < 1 || h->vocab > 1 << 20) return fail(PP_EINVAL, "head: vocab outside [1, 2^20]");
+  if (h->d < 1 || h->d > 1 << 14) return fail(PP_EINVAL, "head: d outside [1, 2^14]");
+  if (top < 0 || top > PP_HEAD_TOP_MAX) return fail(PP_EINVAL, "head: top outside [1, " + std::to_string(PP_HEAD_TOP_MAX) + "]");
+  if (h->dw_lo < 0 || h->dw_hi < h->dw_lo || h->dw_hi > h->vocab) return fail(PP_EINVAL, "head: dw rows outside [0, vocab]");
+  if (h->dw_f32 < 0 || h->dw_f32 > 2) return fail(PP_EINVAL, "head: dw_f32 must be 0, 1 or 2");
+  if (h->piece < 0 || h->piece > 1 << 24) return fail(PP_EINVAL, "head: piece outside [0, 2^24]");
+  const bool dw = h->dw_hi > h->dw_lo;
+  if (h->ldx < h->d || h->ldw < h->d || (h->dx && h->lddx < h->d) || (dw && h->lddw < h->d)) return fail(PP_EINVAL, "head: a leading dimension is smaller than d");
+  if ((h->n > 0 && !h->x) || !h->w || (dw && !h->dw)) return fail(PP_EINVAL, "head: NULL pointer");
+  const uintptr_t al = h->dtype == PP_F32 ? 3 : 1;
+  if (((uintptr_t)h->x | (uintptr_t)h->w | (uintptr_t)h->dx) & al) return fail(PP_EINVAL, "head: x, w or dx is not aligned to its elements");
+  if (dw && (uintptr_t)h->dw & (h->dw_f32 ? 3 : al)) return fail(PP_EINVAL, "head: dw is not aligned to its elements");
+  *a = HeadArgs{h->x, h->w, h->row_weight, h->loss, h->row_loss, h->row_lse, h->dx, dw ? h->dw : nullptr, h->ldx, h->ldw, h->lddx, h->lddw, h->dtype, h->n, h->vocab, h->d,
+                h->dw_lo, h->dw_hi, h->dw_f32, h->piece, nullptr, nullptr, nullptr, top, 1.f, 0.f, nullptr, 0};
+  return PP_OK;
+}
+static int run_head(const char* who, void* hip_stream, const HeadArgs& a, void* ws, size_t ws_bytes) {
+  if (!ws || ((uintptr_t)ws & 255)) return fail(PP_EINVAL, std::string(who) + ": workspace is NULL or not 256-byte aligned");
+  if (ws_bytes < head_bytes(a)) return fail(PP_EINVAL, std::string(who) + ": workspace of " + std::to_string(ws_bytes) + " bytes, needs " + std::to_string(head_bytes(a)) + " (pp_op_head_bytes)");
+  int dev = 0;
+  hipDevice_t own = 0;
+  if (hip_stream) {
+    HIPCHECK(hipGetDevice(&dev));
+    HIPCHECK(hipStreamGetDevice((hipStream_t)hip_stream, &own));
+    if (own != dev) return fail(PP_EINVAL, std::string(who) + ": the stream belongs to another device than the current one");
+  }
+  if (k_head((hipStream_t)hip_stream, a, (char*)ws) != 0) return fail(PP_EHIP, std::string(who) + ": a kernel could not be set up on this device");
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(PP_EHIP, std::string(who) + ": " + hipGetErrorString(e));
+  return PP_OK;
+}
+extern "C" size_t pp_op_head_bytes(const pp_head* head, int32_t top) {
+  HeadArgs a;
+  return check_head(head, top, &a) == PP_OK ? head_bytes(a) : 0;
+}
+extern "C" int pp_op_head_ce(void* hip_stream, const pp_head* head, const int32_t* targets, void* ws, size_t ws_bytes) {
+  HeadArgs a;
+  if (int rc = check_head(head, 0, &a)) return rc;
+  if (a.n > 0 && !targets) return fail(PP_EINVAL, "pp_op_head_ce: targets are NULL");
+  a.targets = targets;
+  return run_head("pp_op_head_ce", hip_stream, a, ws, ws_bytes);
+}
+extern "C" int pp_op_head_distill(void* hip_stream, const pp_head* head, const int32_t* ids, const float* logits, int32_t top, float temperature, float share,
+                                  const int32_t* targets, void* ws, size_t ws_bytes) {
+  HeadArgs a;
+  if (top < 1) return fail(PP_EINVAL, "head: top outside [1, " + std::to_string(PP_HEAD_TOP_MAX) + "]");
+  if (int rc = check_head(head, top, &a)) return rc;
+  if (!(temperature >= 0.015625f && temperature <= 64.f)) return fail(PP_EINVAL, "pp_op_head_distill: temperature outside [2^-6, 2^6]");
+  if (!(share >= 0.f && share <= 1.f)) return fail(PP_EINVAL, "pp_op_head_distill: share outside [0, 1]");
+  if (a.n > 0 && (!ids || !logits || (share < 1.f && !targets))) return fail(PP_EINVAL, "pp_op_head_distill: NULL pointer (targets may be NULL only if share == 1)");
+  a.targets = share < 1.f ? targets : nullptr; a.ids = ids; a.logits = logits; a.tau = temperature; a.share = share;
+  return run_head("pp_op_head_distill", hip_stream, a, ws, ws_bytes);
+}

@@ -121,4 +121,22 @@ int k_attn_bwd_mfma(hipStream_t st, const void* qkv, const void* o, const float*
                     int B, int S, int h, int dh,
                     const float* rope_cos, const float* rope_sin);          // tables given: dq, dk come out w.r.t. the un-rotated q, k
 
+// ---- losses of the output head (pp_head.hip): the operands of one call, checked by the caller (include/pp_ops.h states their meaning)
+struct HeadArgs {
+  const void *x, *w;
+  const float* row_weight;
+  float *loss, *row_loss, *row_lse;
+  void *dx, *dw;
+  int ldx, ldw, lddx, lddw, dtype, n, vocab, d, dw_lo, dw_hi, dw_f32, piece;
+  const int32_t* targets;          // nullptr: no hard targets
+  const int32_t* ids;              // [n x top], top = 0: cross entropy alone
+  const float* logits;
+  int top;
+  float tau, share;                // share of the distillation term (0 where top == 0)
+  const void* wt;                  // W^T [d x vocab] (rows of ldwt) that the caller keeps, or nullptr
+  int ldwt;
+};
+size_t head_bytes(const HeadArgs& a);
+int k_head(hipStream_t st, const HeadArgs& a, char* ws);          // ws: head_bytes(a), 256-byte aligned; 0, or 1 if a kernel cannot be launched
+
 }  // namespace pp
