@@ -84,7 +84,7 @@ typedef struct {
   const void *x, *w;               /* storage type dtype */
   const float* row_weight;         /* [n] or NULL */
   float* loss;                     /* [1] or NULL */
-  float *row_loss, *row_lse;       /* [n] or NULL: l_t; log-sum-exp of z_t / temperature (pp_op_head_ce: of z_t) */
+  float *row_loss, *row_lse;       /* [n] or NULL: l_t; log-sum-exp of z_t / temperature (pp_op_head_ce and share 0: of z_t) */
   void *dx, *dw;                   /* dx [n x d], storage type, or NULL; dw [(dw_hi - dw_lo) x d], or NULL if dw_lo == dw_hi.  Neither may overlap an input. */
   int32_t ldx, ldw, lddx, lddw;    /* elements from row to row, >= d (lddx, lddw: where dx, dw are given) */
   int32_t dtype, n, vocab, d;      /* PP_F32 or PP_BF16; n <= 2^24, vocab <= 2^20, d <= 2^14 */

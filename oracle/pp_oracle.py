@@ -580,6 +580,8 @@ def head_loss(x, w, targets, row_weight=None, ids=None, logits=None, tau=1.0, sh
     n, vocab = x.shape[0], w.shape[0]
     if ids is None:
         tau, share = 1.0, 0.0
+    if share == 0:
+        tau = 1.0
     hard = np.zeros(n, bool) if targets is None or share == 1.0 else (targets >= 0) & (targets < vocab)
     soft = np.zeros(n, bool)
     if ids is not None and share > 0:

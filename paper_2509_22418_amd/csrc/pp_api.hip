@@ -1101,6 +1101,6 @@ extern "C" int pp_op_head_distill(void* hip_stream, const pp_head* head, const i
   if (!(temperature >= 0.015625f && temperature <= 64.f)) return fail(PP_EINVAL, "pp_op_head_distill: temperature outside [2^-6, 2^6]");
   if (!(share >= 0.f && share <= 1.f)) return fail(PP_EINVAL, "pp_op_head_distill: share outside [0, 1]");
   if (a.n > 0 && (!ids || !logits || (share < 1.f && !targets))) return fail(PP_EINVAL, "pp_op_head_distill: NULL pointer (targets may be NULL only if share == 1)");
-  a.targets = share < 1.f ? targets : nullptr; a.ids = ids; a.logits = logits; a.tau = temperature; a.share = share;
+  a.targets = share < 1.f ? targets : nullptr; a.ids = ids; a.logits = logits; a.tau = share > 0.f ? temperature : 1.f; a.share = share;
   return run_head("pp_op_head_distill", hip_stream, a, ws, ws_bytes);
 }

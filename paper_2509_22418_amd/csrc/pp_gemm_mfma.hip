@@ -196,16 +196,29 @@ template <int EPI, bool OUT_F32>
 __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__ B, int ldb,
                                                                void* Cv, int ldc, int M, int N, int Ksplit, const bf16_t* __restrict__ R,
                                                                int tiles_m, int tiles_n, int ldc2,
-                                                               const float* __restrict__ aux0, const float* __restrict__ aux1, int aux_n, int aux_s) {
+                                                               const float* __restrict__ aux0, const float* __restrict__ aux1, int aux_n, int aux_s, HeadEpi he) {
   // EPI_ROPE only: ldc2 = head dim, aux0 / aux1 = cos / sin tables [aux_s x head dim / 2], aux_n = number of leading output
   // columns that are rotated (q and k), aux_s = sequence length (position of row t is t % aux_s)
   extern __shared__ u32x4 lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const int nb = tiles_m * tiles_n;
   const int z = blockIdx.y;
-  const size_t kbase = (size_t)z * Ksplit;
+  int krange = Ksplit;          // of this workgroup
+  size_t kbase = (size_t)z * Ksplit;
+  int live = 0;
+  if constexpr (EPI >= EPI_HEAD_EXP) {
+    if (EPI == EPI_HEAD_EXP && he.redo && he.redo[0] == 0) return;
+    live = min(max(*he.count - he.i0, 0), he.piece);
+    const int live64 = (live + 63) & ~63;
+    int K = aux_n;
+    if (he.rows_are_k) { K = live64; Ksplit = (K / DL_BK + (int)gridDim.y - 1) / (int)gridDim.y * DL_BK; }
+    else { M = live64; tiles_m = (M + BM - 1) / BM; }
+    krange = min(Ksplit, K - z * Ksplit);
+    if (krange <= 0) krange = 0;          // the last ranges may be empty: zeros
+    kbase = krange ? (size_t)z * Ksplit : 0;
+  }
+  const int nb = tiles_m * tiles_n;
   // Tile walk.  The grid's x extent may be smaller than the number of tiles: workgroup b then takes the tiles b,
   // b + gridDim.x, ... one after the other (gridDim.x is a multiple of 8 in that case, so a workgroup's tiles all map to
   // its own XCD below), and requests the first three units of its next tile before it starts the epilogue of the
@@ -251,9 +264,9 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     }
   };
   const int wdst = wave * 32 * 8;          // chunk offset of this wave's rows inside a unit (wave-uniform)
-  const int ns = Ksplit / DL_BK;
+  const int ns = krange / DL_BK;
   auto issue = [&](const bf16_t* const (&g)[4], int s, int slot) {          // unit of super-step s (clamped) into `slot`
-    const size_t koff = (size_t)min(s, ns - 1) * DL_BK;
+    const size_t koff = (size_t)(EPI >= EPI_HEAD_EXP ? max(min(s, ns - 1), 0) : min(s, ns - 1)) * DL_BK;
     u32x4* dst = lds + slot * DL_UNIT_CHUNKS + wdst;
 #pragma unroll
     for (int i = 0; i < 4; ++i) __builtin_amdgcn_global_load_lds(PP_GPTR(g[i] + koff), PP_LPTR(dst + i * 64), 16, 0, 0);
@@ -267,6 +280,20 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   char* const wbase = reinterpret_cast<char*>(lds) + 3 * DL_UNIT_CHUNKS * 16 + wave * 8192;
 
   int vb = blockIdx.x, tm, tn;
+  auto wanted = [&](int b) {          // the first tile from b on that is to be done
+    if constexpr (EPI == EPI_HEAD_EXP)
+      if (he.redo)
+        for (; b < nb; b += gridDim.x) {
+          int m, n;
+          tile_of(b, m, n);
+          if (he.redo[1 + m]) break;
+        }
+    return b;
+  };
+  if constexpr (EPI >= EPI_HEAD_EXP) {
+    vb = wanted(vb);
+    if (vb >= nb) return;
+  }
   tile_of(vb, tm, tn);
   set_ptrs(tm, tn);
   issue(gA, 0, 0); issue(gB, 0, 1); issue(gA, 1, 2);
@@ -354,7 +381,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   // this barrier nobody reads the staged panels any more and nothing is on its way into them
   __builtin_amdgcn_s_waitcnt(0x0070);
   __builtin_amdgcn_s_barrier();
-  const int vb_next = vb + gridDim.x;
+  const int vb_next = wanted(vb + gridDim.x);
   const bool has_next = vb_next < nb;
   int tm_next = 0, tn_next = 0;
   if (has_next) {
@@ -367,7 +394,122 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   // ---- epilogue: element r of accumulator (i, j) is output row m0 + wm*128 + 16 i + lane % 16,
   //      column n0 + wn*64 + 16 j + 4 (lane / 16) + r
   bool stored = false;
-  if constexpr (EPI == EPI_SWIGLU) {
+  if constexpr (EPI == EPI_HEAD_EXP) {
+    // ---- exponentials of a row of logits against the row's reference, their sums and the largest exponent over this wave's 64 columns; see HeadEpi
+    const int grp = tn * 4 + wn, col = n0 + wn * 64 + 4 * lq;
+    bf16_t* C = reinterpret_cast<bf16_t*>(Cv);
+    const bool whole = n0 + wn * 64 + 64 <= N;
+    float rk[8], sum[8], sum2[8], top[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(m0 + wm * 128 + 16 * i + l16, M - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool dead = rk[i] == INFINITY;
+      const float off = -rk[i] * he.k, off2 = -rk[i] * he.kt;
+      float s = 0.f, s2 = 0.f, t = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool out = dead || (!whole && col + 16 * j + r >= N);
+          const float y = out ? -INFINITY : fmaf(acc[i][j][r], he.k, off);
+          if (he.kt != 0.f) s2 += out ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], he.kt, off2));
+          t = fmaxf(t, y);
+          const float e = __builtin_amdgcn_exp2f(y);
+          s += e;
+          acc[i][j][r] = e;
+        }
+      s += __shfl_xor(s, 16, 64); s += __shfl_xor(s, 32, 64);
+      t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
+      if (he.kt != 0.f) { s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64); }
+      sum[i] = s; sum2[i] = s2; top[i] = t;
+    }
+    // every lane has the totals of all 8 row blocks: lane group lq stores blocks lq and lq + 4, 64 consecutive rows each
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      auto pick = [&](const float (&v)[8]) { return lq == 0 ? v[4 * h] : lq == 1 ? v[4 * h + 1] : lq == 2 ? v[4 * h + 2] : v[4 * h + 3]; };
+      const int row = m0 + wm * 128 + 64 * h + lane;
+      if (row < M) {
+        he.stats[(size_t)grp * he.piece + row] = make_float2(pick(sum), pick(top));
+        if (he.kt != 0.f) he.stats2[(size_t)grp * he.piece + row] = pick(sum2);
+      }
+    }
+    if (C && n0 + wn * 64 < he.vp) {
+#pragma unroll
+      for (int hi = 0; hi < 2; ++hi) {          // turned around as in the plain store below
+#pragma unroll
+        for (int ii = 0; ii < 4; ++ii) {
+          const int i = 4 * hi + ii, row = ii * 16 + l16, sw2 = (row >> 1) & 7;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int q = 4 * j + lq;
+            uint2 w;
+            w.x = f32x2_to_bf16x2(acc[i][j][0], acc[i][j][1]);
+            w.y = f32x2_to_bf16x2(acc[i][j][2], acc[i][j][3]);
+            *reinterpret_cast<uint2*>(wbase + row * 128 + (((q >> 1) ^ sw2) << 4) + (q & 1) * 8) = w;
+          }
+        }
+#pragma unroll
+        for (int it = 0; it < 8; ++it) {
+          const int row = 8 * it + (lane >> 3), c = lane & 7;
+          const uint4 v = *reinterpret_cast<const uint4*>(wbase + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
+          const int grow = m0 + wm * 128 + hi * 64 + row;
+          if (grow < M) *reinterpret_cast<uint4*>(C + (size_t)grow * ldc + n0 + wn * 64 + c * 8) = v;
+        }
+      }
+    }
+    stored = true;
+  } else if constexpr (EPI == EPI_HEAD_DX || EPI == EPI_HEAD_DW) {
+    // ---- fp32 patch, 32 rows at a time (as in the residual epilogue below): a lane gets 8 consecutive columns of a row
+#pragma unroll
+    for (int qt = 0; qt < 4; ++qt) {
+#pragma unroll
+      for (int ii = 0; ii < 2; ++ii) {
+        const int i = 2 * qt + ii, row = ii * 16 + l16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<float4*>(wbase + row * 256 + (((4 * j + lq) ^ (row & 15)) << 4)) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+      }
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int row = 8 * it + (lane >> 3), c = lane & 7;
+        const float4 v0 = *reinterpret_cast<const float4*>(wbase + row * 256 + (((2 * c) ^ (row & 15)) << 4));
+        const float4 v1 = *reinterpret_cast<const float4*>(wbase + row * 256 + (((2 * c + 1) ^ (row & 15)) << 4));
+        const int grow = m0 + wm * 128 + qt * 32 + row, gcol = n0 + wn * 64 + c * 8;
+        if (grow >= (EPI == EPI_HEAD_DX ? live : M) || gcol >= N) continue;
+        float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+        size_t off;
+        if constexpr (EPI == EPI_HEAD_DX) {
+          const float sc = he.scale[he.i0 + grow];
+          off = (size_t)he.rows[he.i0 + grow] * ldc + gcol;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= sc;
+        } else {
+          off = (size_t)grow * ldc + gcol;
+          if (he.add) {
+            const float* ad = he.add + (size_t)grow * he.ldadd + gcol;
+            if (he.vec) {
+              float w[8];
+              load8(ad, w);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += w[e];
+            } else
+              for (int e = 0; e < 8 && gcol + e < N; ++e) v[e] += ad[e];
+          }
+        }
+        if (EPI == EPI_HEAD_DW && he.out_f32) {
+          float* o = reinterpret_cast<float*>(Cv) + off;
+          if (he.vec) store8(o, v);
+          else for (int e = 0; e < 8 && gcol + e < N; ++e) o[e] = v[e];
+        } else {
+          bf16_t* o = reinterpret_cast<bf16_t*>(Cv) + off;
+          if (he.vec) store8(o, v);
+          else for (int e = 0; e < 8 && gcol + e < N; ++e) o[e] = from_f32<bf16_t>(v[e]);
+        }
+      }
+    }
+    stored = true;
+  } else if constexpr (EPI == EPI_SWIGLU) {
     // ---- fused SwiGLU epilogue.  acc[i][j] (j = 0, 1) and acc[i][j + 2] are gate and up pre-activations of hidden unit
     // u0 + 16 j + 4 (lane / 16) + r (u0 = tn*128 + wn*32) for output row m0 + wm*128 + 16 i + lane % 16.  Both are
     // rounded to bf16 and stored at columns u and N + u of C (ldc >= 2 N); a = silu(g) * u is formed from the ROUNDED
@@ -638,7 +780,7 @@ static int launch_dl(hipStream_t st, const void* A, int lda, const void* B, int 
   if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
   dim3 grid(splits == 1 ? dl_grid_x(tiles_m * tiles_n) : tiles_m * tiles_n, splits);
-  kern<<<grid, 512, DL_LDS_BYTES, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, C, ldc, M, N, Ksplit, (const bf16_t*)R, tiles_m, tiles_n, 0, nullptr, nullptr, 0, 1);
+  kern<<<grid, 512, DL_LDS_BYTES, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, C, ldc, M, N, Ksplit, (const bf16_t*)R, tiles_m, tiles_n, 0, nullptr, nullptr, 0, 1, HeadEpi{});
   return 0;
 }
 
@@ -672,7 +814,7 @@ int k_gemm_swiglu_fwd_mfma(hipStream_t st, const void* X, int ldx, const void* W
   auto kern = gemm_nt_mfma_dl_kernel<EPI_SWIGLU, false>;
   if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (F + BN / 2 - 1) / (BN / 2);
-  kern<<<dim3(dl_grid_x(tiles_m * tiles_n), 1), 512, DL_LDS_BYTES, st>>>((const bf16_t*)X, ldx, (const bf16_t*)Wgu, ldw, gu, 2 * F, M, F, K, (const bf16_t*)a, tiles_m, tiles_n, F, nullptr, nullptr, 0, 1);
+  kern<<<dim3(dl_grid_x(tiles_m * tiles_n), 1), 512, DL_LDS_BYTES, st>>>((const bf16_t*)X, ldx, (const bf16_t*)Wgu, ldw, gu, 2 * F, M, F, K, (const bf16_t*)a, tiles_m, tiles_n, F, nullptr, nullptr, 0, 1, HeadEpi{});
   return 0;
 }
 
@@ -687,7 +829,7 @@ int k_gemm_swiglu_bwd_mfma(hipStream_t st, const void* G, int ldg, const void* W
   auto kern = gemm_nt_mfma_dl_kernel<EPI_SWIGLU_BWD, false>;
   if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
-  kern<<<dim3(dl_grid_x(tiles_m * tiles_n), 1), 512, DL_LDS_BYTES, st>>>((const bf16_t*)G, ldg, (const bf16_t*)Wd_rows, ldw, dgu_c0, ld2f, M, N, K, (const bf16_t*)gu_c0, tiles_m, tiles_n, half, nullptr, nullptr, 0, 1);
+  kern<<<dim3(dl_grid_x(tiles_m * tiles_n), 1), 512, DL_LDS_BYTES, st>>>((const bf16_t*)G, ldg, (const bf16_t*)Wd_rows, ldw, dgu_c0, ld2f, M, N, K, (const bf16_t*)gu_c0, tiles_m, tiles_n, half, nullptr, nullptr, 0, 1, HeadEpi{});
   return 0;
 }
 
@@ -702,7 +844,7 @@ int k_gemm_qkv_rope_mfma(hipStream_t st, const void* X, int ldx, const void* Wqk
   if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
   const int N = 3 * d, tiles_m = (M + BM - 1) / BM, tiles_n = N / BN;
   kern<<<dim3(dl_grid_x(tiles_m * tiles_n), 1), 512, DL_LDS_BYTES, st>>>((const bf16_t*)X, ldx, (const bf16_t*)Wqkv, ldw, qkv, N, M, N, K, nullptr, tiles_m, tiles_n, dh,
-                                                                         rope_cos, rope_sin, 2 * d, S);
+                                                                         rope_cos, rope_sin, 2 * d, S, HeadEpi{});
   return 0;
 }
 
@@ -741,6 +883,29 @@ int k_gemm_nt_mfma(hipStream_t st, const void* A, int lda, const void* B, int ld
     return 0;
   if (epi == EPI_ADD_RES) return launch<EPI_ADD_RES, false>(st, A, lda, B, ldb, C, ldc, M, N, Ksplit, R, 1);
   return launch<EPI_STORE, false>(st, A, lda, B, ldb, C, ldc, M, N, Ksplit, nullptr, 1);
+}
+
+// ---- the products of the output head's losses
+template <int EPI, bool OUT_F32>
+static int launch_head(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he) {
+  static LdsOptIn opt_in;
+  auto kern = gemm_nt_mfma_dl_kernel<EPI, OUT_F32>;
+  if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
+  const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
+  const int range = (K / DL_BK + splits - 1) / splits * DL_BK;
+  kern<<<dim3(splits == 1 ? dl_grid_x(tiles_m * tiles_n) : tiles_m * tiles_n, splits), 512, DL_LDS_BYTES, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, C, ldc, M, N, range, nullptr, tiles_m, tiles_n,
+                                                                                                               0, nullptr, nullptr, K, 1, he);
+  return 0;
+}
+int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he) {
+  if (M < 1 || N < 1 || K < DL_BK || K % DL_BK || (lda & 7) || (ldb & 7) || splits < 1 || (splits > 1 && epi != EPI_HEAD_PART)) return 1;
+  if (((uintptr_t)A | (uintptr_t)B) & 15) return 1;
+  switch (epi) {
+    case EPI_HEAD_EXP: return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
+    case EPI_HEAD_DX: return launch_head<EPI_HEAD_DX, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
+    case EPI_HEAD_DW: return launch_head<EPI_HEAD_DW, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
+    default: return launch_head<EPI_HEAD_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, splits, he);
+  }
 }
 
 }  // namespace pp

@@ -4,6 +4,17 @@
 // with entries), Q the teacher's q at its entries;  dX = dz W,  dW = dz^T X.
 // Rows that count are gathered into the front of the workspace's copy of X, whose rows are padded with zeros to what the matrix kernels read; every
 // kernel below works on those compact rows, in pieces.
+//
+// bf16: the first product's epilogue stores e = exp((z - r) / tau) instead of z, r a reference of the row that is known BEFORE the product: the largest logit among the target's and
+// the teacher's entries.  A softmax needs no more of its reference than that no exponential overflows or is lost, so the maximum itself is not waited for, and e's rounding to bf16
+// is relative.  With s = sum e the row of dz is a multiple of e but for the target and the entries:
+//     dz = C (e - sub / C),  C = g c / s,  sub = g (c1 [v = y] + ct Q):
+// a kernel over rows replaces e at those few places, and C is applied to dX's rows behind their product and to X's rows in front of dW's.  No other pass over the piece, and no second
+// product of logits: 2 products for dX alone, 3 with dW.  Rows whose largest logit turns out to lie more than kFar above the reference take the maximum, and the first product of
+// their 256-row blocks is done again (by a launch that ends at once where there are none).  Two softmaxes at once (tau != 1 beside hard targets) take one more pass
+// over the piece, which forms the second's exponentials as powers of the first's.
+// Pieces are of rows, not of the vocabulary: a piece of vocabulary would have to wait for the sums of all others, hence form its logits twice (4 products instead of 3), and sum dX in
+// memory.  fp32: logits in fp32, softmax and dz by a block per row, products on the fp32 MFMA kernels.
 #include "pp_kernels.h"
 #include "pp_dev.h"
 
@@ -22,27 +33,46 @@ namespace {
 constexpr int kTopMax = 128;          // entries per row (PP_HEAD_TOP_MAX)
 constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
-  int dp, vp, np, piece;          // padded width, padded vocabulary, rows of the compact X, rows of a piece
-  bool grads, copy_w, own_wt;
-  size_t flags, pos, rows, count, rowl, xc, wc, wt, z, dz, dzt, xt, dxc, dwa, dwp, total;          // byte offsets
+  int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
+  int dx_splits, dw_splits;
+  bool grads, copy_w, own_wt, mixed;
+  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dxc, dwa, dwp, total;          // byte offsets
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
+// K ranges of a product of `tiles` 256 x 256 tiles and `steps` steps of 64: the number that fills rounds of 256 workgroups best.  A tile's step takes about 0.5 us and a workgroup 4 us
+// besides; every range costs a write and a read of the M x N floats (at 4 TB/s).
+int best_splits(long tiles, long steps, double mn) {
+  int best = 1;
+  double cost = 0;
+  for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
+    const double c = (double)((tiles * s + 255) / 256) * (0.5 * ((steps + s - 1) / s) + 4) + (s > 1 ? 4 + s * mn * 8 / 4e6 : 0);
+    if (s == 1 || c < cost) { best = s; cost = c; }
+  }
+  return best;
+}
+
 HeadPlan plan_head(const HeadArgs& a) {
   HeadPlan p{};
-  const size_t es = a.dtype == 0 ? 4 : 2;
-  const int unit = a.dtype == 0 ? 4 : 64;
-  const size_t dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
+  const bool bf = a.dtype != 0;
+  const size_t es = bf ? 2 : 4;
+  const int unit = bf ? 64 : 4;
+  const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
   p.grads = a.dx || a.dw;
+  p.mixed = a.tau != 1.f && a.share > 0.f && a.share < 1.f;
   p.dp = pad_to(a.d, unit);
   p.vp = pad_to(a.vocab, unit);
   p.np = std::max(64, pad_to(a.n, 64));
+  p.groups = (a.vocab + 255) / 256 * 4;
   const size_t row = (size_t)p.vp * es;
   p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(kPieceBytes / row / 256 * 256));
-  p.piece = std::min(p.piece, p.np);
+  p.piece = std::min(std::min(p.piece, p.np), 1 << 18);          // grids of piece / 64 in y
   // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
-  p.copy_w = a.dtype != 0 && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
+  p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !(a.wt && a.vocab % unit == 0 && a.ldwt % 8 == 0 && ((uintptr_t)a.wt & 15) == 0);
+  const long tiles_d = (a.d + 255) / 256;
+  p.dx_splits = bf && a.dx ? best_splits((p.piece + 255) / 256 * tiles_d, p.vp / 64, (double)p.piece * a.d) : 1;
+  p.dw_splits = bf && a.dw ? best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, (double)dw_rows * a.d) : 1;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
   p.flags = take(a.top ? p.np : 0);
@@ -53,13 +83,25 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.xc = take((size_t)p.np * p.dp * es);
   p.wc = take(p.copy_w ? (size_t)a.vocab * p.dp * es : 0);
   p.wt = take(p.own_wt ? (size_t)a.d * p.vp * es : 0);
-  p.z = take((size_t)p.piece * p.vp * 4);
-  p.dz = take(p.grads && a.dtype ? (size_t)p.piece * p.vp * es : 0);          // fp32: in place of z
-  p.dzt = take(a.dw && a.dtype ? dw_rows * p.piece * es : 0);
-  p.xt = take(a.dw && a.dtype ? (size_t)a.d * p.piece * es : 0);
-  p.dxc = take(a.dx ? (size_t)p.piece * p.dp * es : 0);
-  p.dwa = take(dw_rows * a.d * 4);
-  p.dwp = take(p.piece < a.n ? dw_rows * a.d * 4 : 0);
+  if (bf) {
+    p.ref = take((size_t)p.np * 4);
+    p.scale = take((size_t)p.np * 4);
+    p.coef = take(a.top ? (size_t)p.piece * 8 : 0);
+    p.zsel = take((size_t)p.np * (a.top + 1) * 4);
+    p.z = take(p.grads ? (size_t)p.piece * p.vp * es : 0);
+    p.stats = take((size_t)p.groups * p.piece * 8);
+    p.stats2 = take(a.top ? (size_t)p.groups * p.piece * 4 : 0);          // temperature and share are not known where the size is asked for
+    p.redo = take((1 + (size_t)(p.piece + 255) / 256) * 4);
+    p.dzt = take(a.dw ? (size_t)(dw_rows + 8) * p.piece * es : 0);
+    p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
+    p.part = take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
+    p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
+  } else {
+    p.z = take((size_t)p.piece * p.vp * 4);
+    p.dxc = take(a.dx ? (size_t)p.piece * p.dp * es : 0);
+    p.dwa = take((size_t)dw_rows * a.d * 4);
+    p.dwp = take(p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
+  }
   p.total = off;
   return p;
 }
@@ -250,7 +292,300 @@ __global__ __launch_bounds__(256) void head_row_kernel(const float* z_, T* dz_, 
   if (at >= 0) dz[at] = from_f32<T>(own);
 }
 
+// ------------------------------------------------------------------------------------------------ bf16: references, sums, losses and the places that differ
+// zsel[i][j] = z of entry j of compact row i (j == top: of its target) by a wave's dot products in fp32, and ref[i] = the largest of them (inf behind the last row that counts).
+// xc and w rows are dp (a multiple of 64) elements, 16-byte aligned.
+struct HeadRef {
+  const bf16_t *xc, *w;
+  int ldw, dp, np, V, top;
+  const int32_t *rows, *count, *targets, *ids;
+  const float* logits;
+  const unsigned char* flags;
+  float *zsel, *ref;
+};
+__global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (i >= h.np) return;
+  if (i >= *h.count) { if (lane == 0) h.ref[i] = INFINITY; return; }
+  const int t = h.rows[i];
+  const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
+  const bf16_t* x = h.xc + (size_t)i * h.dp;
+  float* zs = h.zsel + (size_t)i * (h.top + 1);
+  float best = -INFINITY;
+  constexpr int NB = 8;          // entries at a time: eight rows of W in flight
+  for (int j0 = soft ? 0 : h.top; j0 <= h.top; j0 += NB) {
+    int id[NB];
+    float s[NB];
+#pragma unroll
+    for (int e = 0; e < NB; ++e) {
+      const int j = j0 + e;
+      id[e] = j < h.top ? h.ids[(size_t)t * h.top + j] : j == h.top && hard ? h.targets[t] : -1;
+      if ((uint32_t)id[e] >= (uint32_t)h.V || (j < h.top && h.logits[(size_t)t * h.top + j] == -INFINITY)) id[e] = -1;
+      s[e] = 0.f;
+    }
+    for (int c = lane * 8; c < h.dp; c += 512) {
+      float xv[8], wv[8];
+      load8(x + c, xv);
+#pragma unroll
+      for (int e = 0; e < NB; ++e)
+        if (id[e] >= 0) {
+          load8(h.w + (size_t)id[e] * h.ldw + c, wv);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[e] = fmaf(xv[k], wv[k], s[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < NB; ++e)
+      if (id[e] >= 0) {
+        const float z = wave_sum(s[e]);
+        if (lane == 0) zs[j0 + e] = z;
+        best = fmaxf(best, z);
+      }
+  }
+  if (lane == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
+}
+
+// A block per 64 compact rows of the piece: sums over the 64-column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
+// entries.  `again`: only rows of blocks that were done again.
+struct HeadFin {
+  const float2* stats;
+  const float* stats2;          // mixed: sums of the second softmax
+  int groups, piece, i0, V, vp, top, mixed, again;
+  const int32_t *rows, *count, *targets, *ids;
+  const float *logits, *weight, *zsel;
+  const unsigned char* flags;
+  float *ref, *scale, *row_loss, *row_lse;
+  float2* coef;                 // mixed: shares of the two exponentials in e, for head_mix_kernel
+  bf16_t* e;                    // nullptr: losses alone
+  int places;                   // 1: the places are written
+  int32_t* redo;
+  float tau, share;
+};
+constexpr float kFar = 40.f;          // e <= exp(40): sums of 2^20 of them, times what dX's product adds up, stay far from overflow, and C far from underflow
+__global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
+  __shared__ float s1_s[16][64], s2_s[16][64], top_s[16][64];
+  __shared__ int id_s[16][kTopMax + 1];
+  __shared__ float q_s[16][kTopMax + 1];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b0 = blockIdx.x * 64, live = min(max(*h.count - h.i0, 0), h.piece);
+  if (h.again) { if (!h.redo[0] || !h.redo[1 + b0 / 256]) return; }
+  if (b0 >= live) return;
+  const int row = b0 + lane;
+  float s1 = 0.f, s2 = 0.f, far = -INFINITY;
+  for (int g = wave; g < h.groups; g += 16) {
+    const float2 v = h.stats[(size_t)g * h.piece + min(row, live - 1)];
+    s1 += v.x;
+    far = fmaxf(far, v.y);
+    if (h.mixed) s2 += h.stats2[(size_t)g * h.piece + min(row, live - 1)];
+  }
+  s1_s[wave][lane] = s1; s2_s[wave][lane] = s2; top_s[wave][lane] = far;
+  __syncthreads();
+  if (wave == 0) {
+    for (int w = 1; w < 16; ++w) { s1 += s1_s[w][lane]; s2 += s2_s[w][lane]; far = fmaxf(far, top_s[w][lane]); }
+    s1_s[0][lane] = s1; s2_s[0][lane] = h.mixed ? s2 : s1;
+    // largest exponent, in units of log 2 of the stored exponential; with two softmaxes the second's may be larger
+    const bool single_tau = !h.mixed;
+    const float k = 1.44269504f / (single_tau ? h.tau : 1.f), span = far * 0.693147181f * (single_tau ? 1.f : fmaxf(1.f, 1.f / h.tau));
+    if (!h.again && row < live && span > kFar && far < 1e30f) {
+      h.ref[h.i0 + row] += far / k;
+      h.redo[0] = 1;
+      h.redo[1 + b0 / 256] = 1;
+    }
+  }
+  __syncthreads();
+  for (int r = wave; r < 64 && b0 + r < live; r += 16) {
+    const int i = h.i0 + b0 + r, t = h.rows[i];
+    const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
+    const float ref = h.ref[i], it = 1.0f / h.tau;
+    const float sa = s1_s[0][r], st = s2_s[0][r];          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
+    const float* zs = h.zsel + (size_t)i * (h.top + 1);
+    const int y = hard ? h.targets[t] : -1;
+    const float zy = hard ? zs[h.top] : 0.f;
+    // the teacher's softmax over its entries, two per lane
+    int id[2] = {-1, -1};
+    float q[2] = {0.f, 0.f}, zj[2] = {0.f, 0.f};
+    float l = 0.f;
+    if (soft) {
+      float u[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int j = lane + 64 * k;
+        if (j < h.top) {
+          id[k] = h.ids[(size_t)t * h.top + j];
+          if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j] * it; else id[k] = -1;
+          if (u[k] == -INFINITY) id[k] = -1;
+          if (id[k] >= 0) zj[k] = zs[j];
+        }
+      }
+      const float m = wave_max(fmaxf(id[0] >= 0 ? u[0] : -INFINITY, id[1] >= 0 ? u[1] : -INFINITY));
+#pragma unroll
+      for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf(u[k] - m) : 0.f;
+      const float sum = wave_sum(q[0] + q[1]), lst = logf(st);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        q[k] /= sum;
+        if (id[k] >= 0 && !(q[k] <= 0.f)) l += q[k] * (logf(q[k]) - (zj[k] - ref) * it + lst);
+      }
+      l = wave_sum(l) * h.share * h.tau * h.tau;
+    }
+    if (hard) l += (1.f - h.share) * ((ref - zy) + logf(sa));
+    if (lane == 0) {
+      h.row_loss[t] = l;
+      if (h.row_lse) h.row_lse[t] = ref * it + logf(st);
+    }
+    if (!h.e) continue;
+    const float g = h.weight ? h.weight[t] : 1.0f / (float)*h.count;
+    const float c1 = hard ? g * (1.f - h.share) : 0.f, ct = soft ? g * h.share * h.tau : 0.f;
+    const float p1 = c1 / sa, pt = ct / st, C = p1 + pt;          // dz = p1 e1 + pt et - sub
+    const float inv = C != 0.f ? 1.0f / C : 0.f;
+    if (h.coef && lane == 0) h.coef[b0 + r] = make_float2(p1 * inv, pt * inv);
+    if (!h.places) continue;
+    // e at the places, in fp32: the softmaxes' part from the place's logit, less what is taken off there.  The first of equal ids stands for all, in their order; lane 0
+    // holds the target in its third slot unless it is among the entries.
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (lane + 64 * k < h.top) { id_s[wave][lane + 64 * k] = id[k]; q_s[wave][lane + 64 * k] = q[k]; }
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): this wave's own list
+    auto place = [&](float zv, float sub) {
+      const float e1 = p1 != 0.f ? p1 * expf((zv - ref) * (h.mixed ? 1.f : it)) : 0.f, et = pt != 0.f ? pt * expf((zv - ref) * it) : 0.f;
+      return (e1 + et - sub) * inv;
+    };
+    int at[3] = {-1, -1, -1};
+    float val[3] = {0.f, 0.f, 0.f};
+    bool y_listed = false;
+    if (soft)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int j = lane + 64 * k;
+        if (j < h.top && id[k] >= 0) {
+          bool first = true;
+          float sub = id[k] == y ? c1 : 0.f;
+          y_listed |= id[k] == y;
+          for (int o = 0; o < h.top; ++o)
+            if (id_s[wave][o] == id[k]) { if (o < j) first = false; sub += ct * q_s[wave][o]; }
+          if (first) { at[k] = id[k]; val[k] = place(zj[k], sub); }
+        }
+      }
+    if (hard && !__ballot(y_listed) && lane == 0) { at[2] = y; val[2] = place(zy, c1); }
+    // The row of dz is C e.  Most of its length lies in the largest place (at the target p - 1 against many small p), so C is moved by the at most 2^-8 that make that place's rounded
+    // value exact, and the rounding error of the whole gradient is that of its smaller part (128 x 2048, vocab 32000: dX 2.4e-3 -> 1.8e-3 from the exact values, 1.7e-3 of it its own
+    // rounding).
+    float big = fmaxf(fmaxf(fabsf(val[0]), fabsf(val[1])), fabsf(val[2]));
+    big = wave_max(big);
+    const float rounded = bf16_to_f32(f32_to_bf16(big));
+    const float move = big > 0.f && big < 1e37f ? rounded / big : 1.f;          // exact e -> stored e
+    if (lane == 0) h.scale[i] = C / move;
+    bf16_t* e = h.e + (size_t)(b0 + r) * h.vp;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (at[k] >= 0) e[at[k]] = from_f32<bf16_t>(val[k] * move);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Two softmaxes: e1 = exp(z - r) becomes (p1 e1 + pt e1^(1 / tau)) / C, in front of head_fin's places.  The power's argument lies within a row's rounded e1; its relative error is 1 / tau of it.
+__global__ __launch_bounds__(256) void head_mix_kernel(bf16_t* e, int vp, const float2* __restrict__ coef, const int32_t* __restrict__ count, int i0, int piece, float it) {
+  const int i = blockIdx.x;
+  if (i >= min(max(*count - i0, 0), piece)) return;
+  const float2 c = coef[i];
+  uint4* row = reinterpret_cast<uint4*>(e + (size_t)i * vp);
+  for (int v = threadIdx.x; v < vp / 8; v += 256) {
+    uint4 r = row[v];
+    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float a = __uint_as_float(w[k] << 16), b = __uint_as_float(w[k] & 0xffff0000u);
+      // e1 = 0 (lost, or behind the vocabulary): log2 = -inf, power 0
+      w[k] = f32x2_to_bf16x2(c.x * a + c.y * __builtin_amdgcn_exp2f(it * __builtin_amdgcn_logf(a)), c.x * b + c.y * __builtin_amdgcn_exp2f(it * __builtin_amdgcn_logf(b)));
+    }
+    row[v] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// dst[c][i] = scale[i] x[i][c] for the compact rows of a piece (live64 of them): X's rows as dW's product reads them
+__global__ __launch_bounds__(256) void head_xt_kernel(const bf16_t* __restrict__ x, int dp, const float* __restrict__ scale, bf16_t* __restrict__ dst, int ld_dst, int d, const int32_t* __restrict__ count,
+                                                      int i0, int piece) {
+  __shared__ uint16_t tile[64][72];
+  const int live = min(max(*count - i0, 0), piece), r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, t = threadIdx.x;
+  if (r0 >= live) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = (t >> 3) + 32 * i, c8 = (t & 7) * 8;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (r0 + r < live) {
+      load8(x + (size_t)(r0 + r) * dp + c0 + c8, v);
+      const float s = scale[i0 + r0 + r];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= s;
+    }
+    store8(reinterpret_cast<bf16_t*>(&tile[r][c8]), v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = (t >> 3) + 32 * i, r8 = (t & 7) * 8;
+    if (c0 + c >= d) continue;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r8 + 2 * k][c] | ((uint32_t)tile[r8 + 2 * k + 1][c] << 16);
+    *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+// dst[v - v0][i] = e[i][v] for v0 <= v < v1 (v0 a multiple of 8) and the compact rows of a piece, zeros for rows behind the last one that counts
+__global__ __launch_bounds__(256) void head_et_kernel(const bf16_t* __restrict__ e, int vp, int v0, int v1, bf16_t* __restrict__ dst, int ld_dst, const int32_t* __restrict__ count, int i0, int piece) {
+  __shared__ uint16_t tile[64][72];
+  const int live = min(max(*count - i0, 0), piece), r0 = blockIdx.y * 64, c0 = v0 + blockIdx.x * 64, t = threadIdx.x;
+  if (r0 >= live) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = (t >> 3) + 32 * i, c8 = (t & 7) * 8;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r0 + r < live && c0 + c8 < vp) v = *reinterpret_cast<const uint4*>(e + (size_t)(r0 + r) * vp + c0 + c8);
+    *reinterpret_cast<uint4*>(&tile[r][c8]) = v;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = (t >> 3) + 32 * i, r8 = (t & 7) * 8;
+    if (c0 + c >= v1) continue;
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r8 + 2 * k][c] | ((uint32_t)tile[r8 + 2 * k + 1][c] << 16);
+    *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c - v0) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+__global__ void head_clear_kernel(int32_t* p, int n) {
+  for (int i = threadIdx.x; i < n; i += 256) p[i] = 0;
+}
+
 // ------------------------------------------------------------------------------------------------ outputs
+// dx[rows[i]] = scale[i] sum of the partials [splits][live64][d], a wave per compact row of the piece
+__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const float* __restrict__ scale, bf16_t* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows,
+                                                          const int32_t* __restrict__ count, int i0, int piece) {
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), live = min(max(*count - i0, 0), piece);
+  if (i >= live) return;
+  const size_t mn = (size_t)((live + 63) & ~63) * d;
+  const float sc = scale[i0 + i];
+  const int t = rows[i0 + i];
+  for (int c = threadIdx.x & 63; c < d; c += 64) {
+    float s = 0.f;
+    for (int z = 0; z < splits; ++z) s += part[z * mn + (size_t)i * d + c];
+    dx[(size_t)t * lddx + c] = from_f32<bf16_t>(s * sc);
+  }
+}
+// out = sum of the partials [splits][rows][d] (+ add), out float or bf16
+template <class TO>
+__global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restrict__ part, int splits, const float* add, int ldadd, TO* out, int ldo, int rows, int d) {
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= rows) return;
+  for (int c = threadIdx.x & 63; c < d; c += 64) {
+    float s = 0.f;
+    for (int z = 0; z < splits; ++z) s += part[(size_t)z * rows * d + (size_t)r * d + c];
+    if (add) s += add[(size_t)r * ldadd + c];
+    out[(size_t)r * ldo + c] = from_f32<TO>(s);
+  }
+}
 // dx[rows[i]] = dxc[i] for the compact rows of a piece
 template <class T>
 __global__ __launch_bounds__(256) void head_scatter_kernel(const T* __restrict__ dxc, int dp, T* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows, const int32_t* __restrict__ count,
@@ -282,16 +617,116 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(const float* __restrict
 }
 
 // ------------------------------------------------------------------------------------------------ one call
+static dim3 quads(int rows) { return dim3((rows + 3) / 4); }
+
+static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, const void* w, int ldw, const void* wt, int ldwt, float* row_loss) {
+  const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
+  auto* rows = (int32_t*)(ws + p.rows);
+  auto* count = (int32_t*)(ws + p.count);
+  float *dwa = (float*)(ws + p.dwa), *z = (float*)(ws + p.z), *dxc = (float*)(ws + p.dxc);
+  HeadRow h{rows, count, a.targets, a.ids, a.logits, a.row_weight, a.top ? (unsigned char*)(ws + p.flags) : nullptr, row_loss, a.row_lse, a.tau, a.share, a.vocab, p.vp, a.top, 0};
+  for (int i0 = 0; i0 < a.n; i0 += p.piece) {
+    const int m = std::min(p.piece, p.np - i0);
+    const float* xp = (const float*)(ws + p.xc) + (size_t)i0 * p.dp;
+    auto nt = [&](const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K) { k_gemm_nt_f32(st, 0, A, lda, B, ldb, C, ldc, M, N, K, EPI_STORE, nullptr, 1, 1, nullptr); };
+    h.i0 = i0;
+    nt(xp, p.dp, w, ldw, z, p.vp, m, a.vocab, a.d);
+    head_row_kernel<float><<<m, 256, 0, st>>>(z, p.grads ? z : nullptr, h);
+    if (a.dx) {
+      nt(z, p.vp, wt, ldwt, dxc, p.dp, m, a.d, a.vocab);
+      head_scatter_kernel<float><<<quads(m), 256, 0, st>>>(dxc, p.dp, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
+    }
+    if (a.dw) {
+      const bool first = i0 == 0, last = i0 + p.piece >= a.n;
+      float* prod = first ? dwa : (float*)(ws + p.dwp);
+      // columns that start off a group of four, or rows too long for the token-major kernel's offsets, cannot happen: vp <= 2^20 + 3
+      k_gemm_tn_f32(st, z + a.dw_lo, p.vp, dw_rows, 0, xp, p.dp, prod, a.d, dw_rows, a.d, m, 1, nullptr);
+      if (!first) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(prod, dwa, a.d, dw_rows, a.d, 1);
+      if (last) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(dwa, (float*)a.dw, a.lddw, dw_rows, a.d, a.dw_f32 == 2);
+    }
+  }
+}
+
+static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, const void* w, int ldw, const void* wt, int ldwt, float* row_loss) {
+  const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
+  auto* rows = (int32_t*)(ws + p.rows);
+  auto* count = (int32_t*)(ws + p.count);
+  auto* flags = a.top ? (unsigned char*)(ws + p.flags) : nullptr;
+  float *ref = (float*)(ws + p.ref), *scale = (float*)(ws + p.scale), *zsel = (float*)(ws + p.zsel), *part = (float*)(ws + p.part);
+  auto* stats = (float2*)(ws + p.stats);
+  auto* stats2 = (float*)(ws + p.stats2);
+  auto* redo = (int32_t*)(ws + p.redo);
+  auto* coef = p.mixed ? (float2*)(ws + p.coef) : nullptr;
+  bf16_t* e = p.grads ? (bf16_t*)(ws + p.z) : nullptr;
+  const bf16_t* xc = (const bf16_t*)(ws + p.xc);
+  bool ok = true;
+  head_ref_kernel<<<quads(p.np), 256, 0, st>>>(HeadRef{xc, (const bf16_t*)w, ldw, p.dp, p.np, a.vocab, a.top, rows, count, a.targets, a.ids, a.logits, flags, zsel, ref});
+  const float log2e = 1.44269504f;
+  for (int i0 = 0; i0 < a.n; i0 += p.piece) {
+    const int m = std::min(p.piece, p.np - i0);          // a multiple of 64
+    const bf16_t* xp = xc + (size_t)i0 * p.dp;
+    HeadEpi he{};
+    he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp;
+    HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
+              !p.mixed, redo, a.tau, a.share};
+    head_clear_kernel<<<1, 256, 0, st>>>(redo, 1 + (m + 255) / 256);
+    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
+    head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+    he.redo = redo;
+    f.again = 1;
+    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
+    head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+    if (!e) continue;
+    if (p.mixed) {
+      head_mix_kernel<<<m, 256, 0, st>>>(e, p.vp, coef, count, i0, m, 1.0f / a.tau);
+      f.again = 0; f.places = 1;
+      head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+    }
+    he.scale = scale; he.rows = rows;
+    if (a.dx) {
+      he.vec = a.d % 8 == 0 && a.lddx % 8 == 0 && ((uintptr_t)a.dx & 15) == 0;
+      if (p.dx_splits == 1)
+        ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, wt, ldwt, a.dx, a.lddx, m, a.d, p.vp, 1, he) == 0;
+      else {
+        ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, p.dx_splits, he) == 0;
+        head_dx_sum_kernel<<<quads(m), 256, 0, st>>>(part, p.dx_splits, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
+      }
+    }
+    if (a.dw) {
+      const bool first = i0 == 0, last = i0 + p.piece >= a.n;
+      const int v0 = a.dw_lo & ~7;
+      bf16_t *et = (bf16_t*)(ws + p.dzt), *xt = (bf16_t*)(ws + p.xt);
+      head_xt_kernel<<<dim3(m / 64, p.dp / 64), 256, 0, st>>>(xp, p.dp, scale, xt, p.piece, a.d, count, i0, m);
+      head_et_kernel<<<dim3((a.dw_hi - v0 + 63) / 64, m / 64), 256, 0, st>>>(e, p.vp, v0, a.dw_hi, et, p.piece, count, i0, m);
+      et += (size_t)(a.dw_lo - v0) * p.piece;
+      // the sums of several pieces are kept in fp32: in dw itself where that is float, else in the workspace until the last
+      float* acc = a.dw_f32 ? (float*)a.dw : (float*)(ws + p.dwa);
+      const int ldacc = a.dw_f32 ? a.lddw : a.d;
+      he.rows_are_k = 1;
+      he.add = !first || a.dw_f32 == 2 ? acc : nullptr; he.ldadd = ldacc;
+      he.out_f32 = a.dw_f32 || !last;
+      void* out = he.out_f32 ? (void*)acc : a.dw;
+      const int ldo = he.out_f32 ? ldacc : a.lddw;
+      he.vec = a.d % 8 == 0 && ldo % 8 == 0 && (!he.add || ldacc % 8 == 0) && (((uintptr_t)out | (uintptr_t)he.add) & 15) == 0;
+      if (p.dw_splits == 1)
+        ok &= k_head_gemm(st, EPI_HEAD_DW, et, p.piece, xt, p.piece, out, ldo, dw_rows, a.d, m, 1, he) == 0;
+      else {
+        ok &= k_head_gemm(st, EPI_HEAD_PART, et, p.piece, xt, p.piece, part, a.d, dw_rows, a.d, m, p.dw_splits, he) == 0;
+        if (he.out_f32) head_dw_sum_kernel<float><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (float*)out, ldo, dw_rows, a.d);
+        else head_dw_sum_kernel<bf16_t><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (bf16_t*)out, ldo, dw_rows, a.d);
+      }
+    }
+  }
+  return ok;
+}
+
 int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   const HeadPlan p = plan_head(a);
   const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
-  const size_t es = a.dtype == 0 ? 4 : 2;
-  auto quads = [](int rows) { return dim3((rows + 3) / 4); };
   auto* pos = (int32_t*)(ws + p.pos);
   auto* rows = (int32_t*)(ws + p.rows);
   auto* count = (int32_t*)(ws + p.count);
   auto* flags = a.top ? (unsigned char*)(ws + p.flags) : nullptr;
-  auto* dwa = (float*)(ws + p.dwa);
   float* row_loss = a.row_loss ? a.row_loss : (float*)(ws + p.rowl);
   char* xc = ws + p.xc;
 
@@ -311,45 +746,13 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   };
   if (p.own_wt) { transpose(a.w, a.ldw, ws + p.wt, p.vp, a.vocab, a.d); wt = ws + p.wt; ldwt = p.vp; }
 
-  HeadRow h{rows, count, a.targets, a.ids, a.logits, a.row_weight, flags, row_loss, a.row_lse, a.tau, a.share, a.vocab, p.vp, a.top, 0};
-  bool ok = true;
   if (a.n == 0 && a.dw && a.dw_f32 != 2) {
     if (a.dw_f32) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(nullptr, (float*)a.dw, a.lddw, dw_rows, a.d, 0);
     else PP_H_DISPATCH(a.dtype, head_add_kernel<T><<<quads(dw_rows), 256, 0, st>>>(nullptr, (T*)a.dw, a.lddw, dw_rows, a.d, 0));
   }
-  for (int i0 = 0; i0 < a.n; i0 += p.piece) {
-    const int m = std::min(p.piece, p.np - i0);          // a multiple of 64
-    const char* xp = xc + (size_t)i0 * p.dp * es;
-    float* z = (float*)(ws + p.z);
-    char* dz = a.dtype ? ws + p.dz : ws + p.z;
-    h.i0 = i0;
-    auto nt = [&](const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int out_f32) {
-      if (a.dtype) ok &= k_gemm_nt_mfma(st, A, lda, B, ldb, C, ldc, M, N, K, EPI_STORE, nullptr, out_f32, 1, nullptr) == 0;
-      else k_gemm_nt_f32(st, 0, A, lda, B, ldb, C, ldc, M, N, K, EPI_STORE, nullptr, 1, 1, nullptr);
-    };
-    nt(xp, p.dp, w, ldw, z, p.vp, m, a.vocab, a.dtype ? p.dp : a.d, 1);
-    PP_H_DISPATCH(a.dtype, head_row_kernel<T><<<m, 256, 0, st>>>(z, p.grads ? (T*)dz : nullptr, h));
-    if (a.dx) {
-      nt(dz, p.vp, wt, ldwt, ws + p.dxc, p.dp, m, a.d, a.dtype ? p.vp : a.vocab, 0);
-      PP_H_DISPATCH(a.dtype, head_scatter_kernel<T><<<quads(m), 256, 0, st>>>((const T*)(ws + p.dxc), p.dp, (T*)a.dx, a.lddx, a.d, rows, count, i0, m));
-    }
-    if (a.dw) {
-      const char* dzs = dz + (size_t)a.dw_lo * es;
-      const bool first = i0 == 0, last = i0 + p.piece >= a.n;
-      float* prod = first ? dwa : (float*)(ws + p.dwp);
-      if (a.dtype) {
-        transpose(dzs, p.vp, ws + p.dzt, p.piece, m, dw_rows);
-        transpose(xp, p.dp, ws + p.xt, p.piece, m, a.d);
-        nt(ws + p.dzt, p.piece, ws + p.xt, p.piece, prod, a.d, dw_rows, a.d, m, 1);
-      } else
-        ok &= k_gemm_tn_f32(st, (const float*)dzs, p.vp, dw_rows, 0, (const float*)xp, p.dp, prod, a.d, dw_rows, a.d, m, 1, nullptr) == 0;
-      if (!first) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(prod, dwa, a.d, dw_rows, a.d, 1);
-      if (last) {
-        if (a.dw_f32) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(dwa, (float*)a.dw, a.lddw, dw_rows, a.d, a.dw_f32 == 2);
-        else PP_H_DISPATCH(a.dtype, head_add_kernel<T><<<quads(dw_rows), 256, 0, st>>>(dwa, (T*)a.dw, a.lddw, dw_rows, a.d, 0));
-      }
-    }
-  }
+  bool ok = true;
+  if (a.dtype) ok = head_bf16(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
+  else head_f32(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
   if (a.loss) head_loss_kernel<<<1, 1024, 0, st>>>(row_loss, a.row_weight, pos, count, a.loss, a.n);
   return ok ? 0 : 1;
 }

@@ -18,7 +18,8 @@ struct ShadowSeg {      // one trainable row block that also lives, transposed, 
   int32_t rows, cols, shadow_ld, tile_start;   // tile_start: first 64x64 tile index of this block in the batched launch
 };
 
-enum { EPI_STORE = 0, EPI_ADD_RES = 1, EPI_SWIGLU = 2, EPI_SWIGLU_BWD = 3, EPI_ROPE = 4 };          // the last three: only inside k_gemm_swiglu_*_mfma / k_gemm_qkv_rope_mfma
+enum { EPI_STORE = 0, EPI_ADD_RES = 1, EPI_SWIGLU = 2, EPI_SWIGLU_BWD = 3, EPI_ROPE = 4,          // the last three: only inside k_gemm_swiglu_*_mfma / k_gemm_qkv_rope_mfma
+       EPI_HEAD_EXP = 5, EPI_HEAD_DX = 6, EPI_HEAD_DW = 7, EPI_HEAD_PART = 8 };                    // only inside k_head_gemm
 
 void k_fill_f32(hipStream_t st, float* p, size_t n, float v);
 void k_rope_tables(hipStream_t st, float* cosb, float* sinb, int S, int dh, float base);
@@ -136,6 +137,31 @@ struct HeadArgs {
   const void* wt;                  // W^T [d x vocab] (rows of ldwt) that the caller keeps, or nullptr
   int ldwt;
 };
+// What the head's products on the bf16 matrix cores read besides their operands.  The number of rows that count is on the device only: live = clamp(*count - i0, 0, piece), and
+// whole groups of 64 rows are worked on (rows behind the last one that counts are zeros in every operand).
+struct HeadEpi {
+  const int32_t* count;
+  int i0, piece;
+  int rows_are_k;                  // 0: the rows are the product's rows (M = live), 1: its contraction index (K = live)
+  // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and 64 columns the sum of e, the largest exponent and, where kt != 0, the sum of
+  // exp2(kt (z - ref)), at [64-column group][row of the piece].  A row with ref = inf gives e = 0.
+  const float* ref;
+  float2* stats;
+  float* stats2;
+  float k, kt;
+  int vp;
+  const int32_t* redo;             // nullptr, or: [0] != 0 if any, [1 + b] != 0 if rows 256 b .. are to be done (nothing else is)
+  // EPI_HEAD_DX: row i of the product times scale[i] goes to row rows[i] of C
+  const float* scale;
+  const int32_t* rows;
+  // EPI_HEAD_DW: C = product (+ add), C float (out_f32) or bf16
+  const float* add;
+  int ldadd, out_f32;
+  int vec;                         // DX, DW: rows of C (and add) are whole aligned groups of 8
+};
+// C = A[M x K] B[N x K]^T on 256 x 256 tiles, epi one of EPI_HEAD_*; splits > 1 (EPI_HEAD_PART): float partials [splits][M][N] to C.  M (or K) is the piece's size where it is
+// the rows that count.  Returns 0 if launched, 1 if not.
+int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he);
 size_t head_bytes(const HeadArgs& a);
 int k_head(hipStream_t st, const HeadArgs& a, char* ws);          // ws: head_bytes(a), 256-byte aligned; 0, or 1 if a kernel cannot be launched
 

@@ -63,7 +63,8 @@ def call(x, w, y, ids=None, u=None, tau=1.0, share=1.0, weight=None, dx=True, dw
 def check(got, x, w, y, ids=None, u=None, tau=1.0, share=1.0, weight=None, dw=None, base=0.0):
     """Every output within bounds summed from the roundings on its way:
     z: fp32 sums of d products; an exponential of an argument of size A: A + 8 roundings; a row's sum: at most vocab / 64 + 64 additions one after the other; bf16: the
-    exponentials (half a step, 2^-8) and the scaled rows of X (2^-8) that enter the gradients' products, and the outputs' own rounding (2^-8)."""
+    exponentials (half a step, 2^-8) and the scaled rows of X (2^-8) that enter the gradients' products, the outputs' own rounding (2^-8), and a row's scale, which is chosen for its
+    largest place to come out exact: a relative change of at most half a step (2^-8) of everything else in the row, so 2 * 2^-8 before the products."""
     np64 = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
     ints = lambda t: None if t is None else t.long().cpu().numpy()  # noqa: E731
     X, W, wt = np64(x), np64(w), np64(weight)
@@ -88,7 +89,7 @@ def check(got, x, w, y, ids=None, u=None, tau=1.0, share=1.0, weight=None, dw=No
     assert abs(got["loss"][0] - ref["loss"]) <= np.sum(np.abs(g) * (tol_row + (n / 256 + 40) * EPS * np.abs(ref["row_loss"]))) + 1e-30, "loss"
     # |dz| before its parts cancel: the softmaxes (vocabulary) and what is taken off at the target and the entries
     part = np.abs(ref["dz"])
-    ez_rel = 2 * rel[:, None] + half + (8 * EPS)
+    ez_rel = 2 * rel[:, None] + 2 * half + (8 * EPS)
     off = np.zeros_like(part)          # absolute error where p and the taken-off part cancel: fp32 roundings of parts of size g
     if share < 1.0:
         Y = ints(y)
