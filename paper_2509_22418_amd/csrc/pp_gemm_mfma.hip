@@ -396,53 +396,63 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   bool stored = false;
   if constexpr (EPI == EPI_HEAD_EXP) {
     // ---- exponentials of a row of logits against the row's reference, their sums and the largest exponent over this wave's 64 columns; see HeadEpi
-    const int grp = tn * 4 + wn, col = n0 + wn * 64 + 4 * lq;
+    // (the lane index is laundered as in the rotary epilogue: its addresses are formed here, not above the main loop)
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int e16 = ln & 15, eq = ln >> 4, grp = tn * 4 + wn;
     bf16_t* C = reinterpret_cast<bf16_t*>(Cv);
-    const bool whole = n0 + wn * 64 + 64 <= N;
-    float rk[8], sum[8], sum2[8], top[8];
+    if (n0 + wn * 64 + 64 > N) {          // columns behind the vocabulary
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(m0 + wm * 128 + 16 * i + l16, M - 1)];
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n0 + wn * 64 + 16 * j + 4 * eq + r >= N)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i][j][r] = -INFINITY;
+    }
+    const int row0 = m0 + wm * 128 + e16;
+    float rk[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(row0 + 16 * i, M - 1)];
+    if (he.kt != 0.f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float off2 = -rk[i] * he.kt;
+        float s2 = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s2 += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], he.kt, off2));
+        s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64);
+        if (eq == 0 && row0 + 16 * i < M) he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = s2;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const bool dead = rk[i] == INFINITY;
-      const float off = -rk[i] * he.k, off2 = -rk[i] * he.kt;
-      float s = 0.f, s2 = 0.f, t = -INFINITY;
+      const float off = -rk[i] * he.k;
+      float s = 0.f, t = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool out = dead || (!whole && col + 16 * j + r >= N);
-          const float y = out ? -INFINITY : fmaf(acc[i][j][r], he.k, off);
-          if (he.kt != 0.f) s2 += out ? 0.f : __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], he.kt, off2));
+          const float y = fmaf(acc[i][j][r], he.k, off);
           t = fmaxf(t, y);
-          const float e = __builtin_amdgcn_exp2f(y);
-          s += e;
-          acc[i][j][r] = e;
+          acc[i][j][r] = __builtin_amdgcn_exp2f(y);
+          s += acc[i][j][r];
         }
       s += __shfl_xor(s, 16, 64); s += __shfl_xor(s, 32, 64);
       t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
-      if (he.kt != 0.f) { s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64); }
-      sum[i] = s; sum2[i] = s2; top[i] = t;
-    }
-    // every lane has the totals of all 8 row blocks: lane group lq stores blocks lq and lq + 4, 64 consecutive rows each
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      auto pick = [&](const float (&v)[8]) { return lq == 0 ? v[4 * h] : lq == 1 ? v[4 * h + 1] : lq == 2 ? v[4 * h + 2] : v[4 * h + 3]; };
-      const int row = m0 + wm * 128 + 64 * h + lane;
-      if (row < M) {
-        he.stats[(size_t)grp * he.piece + row] = make_float2(pick(sum), pick(top));
-        if (he.kt != 0.f) he.stats2[(size_t)grp * he.piece + row] = pick(sum2);
-      }
+      if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
     }
     if (C && n0 + wn * 64 < he.vp) {
 #pragma unroll
       for (int hi = 0; hi < 2; ++hi) {          // turned around as in the plain store below
 #pragma unroll
         for (int ii = 0; ii < 4; ++ii) {
-          const int i = 4 * hi + ii, row = ii * 16 + l16, sw2 = (row >> 1) & 7;
+          const int i = 4 * hi + ii, row = ii * 16 + e16, sw2 = (row >> 1) & 7;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int q = 4 * j + lq;
+            const int q = 4 * j + eq;
             uint2 w;
             w.x = f32x2_to_bf16x2(acc[i][j][0], acc[i][j][1]);
             w.y = f32x2_to_bf16x2(acc[i][j][2], acc[i][j][3]);
@@ -451,7 +461,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         }
 #pragma unroll
         for (int it = 0; it < 8; ++it) {
-          const int row = 8 * it + (lane >> 3), c = lane & 7;
+          const int row = 8 * it + (ln >> 3), c = ln & 7;
           const uint4 v = *reinterpret_cast<const uint4*>(wbase + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
           const int grow = m0 + wm * 128 + hi * 64 + row;
           if (grow < M) *reinterpret_cast<uint4*>(C + (size_t)grow * ldc + n0 + wn * 64 + c * 8) = v;

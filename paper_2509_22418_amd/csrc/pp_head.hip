@@ -34,7 +34,7 @@ constexpr int kTopMax = 128;          // entries per row (PP_HEAD_TOP_MAX)
 constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
   int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
-  int dx_splits, dw_splits;
+  int dx_splits, dw_splits, n_redo;
   bool grads, copy_w, own_wt, mixed;
   size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dxc, dwa, dwp, total;          // byte offsets
 };
@@ -91,7 +91,8 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.z = take(p.grads ? (size_t)p.piece * p.vp * es : 0);
     p.stats = take((size_t)p.groups * p.piece * 8);
     p.stats2 = take(a.top ? (size_t)p.groups * p.piece * 4 : 0);          // temperature and share are not known where the size is asked for
-    p.redo = take((1 + (size_t)(p.piece + 255) / 256) * 4);
+    p.n_redo = (p.np + p.piece - 1) / p.piece * (1 + (p.piece + 255) / 256);
+    p.redo = take((size_t)p.n_redo * 4);
     p.dzt = take(a.dw ? (size_t)(dw_rows + 8) * p.piece * es : 0);
     p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
     p.part = take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
@@ -124,20 +125,40 @@ __global__ __launch_bounds__(256) void head_flags_kernel(const int32_t* __restri
   if (lane == 0) flags[t] = weight && weight[t] == 0.f ? 0 : (hard_row(targets, t, V) ? ROW_HARD : 0) | (soft ? ROW_SOFT : 0);
 }
 
-// pos[t] = place of row t among the rows that count, -1 for the others; rows[i] = t; count = their number.  One block; 16 consecutive rows per thread.
+// pos[t] = place of row t among the rows that count, -1 for the others; rows[i] = t; count = their number; redo cleared.  One block; 16 consecutive rows per thread.
 __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restrict__ targets, const unsigned char* __restrict__ flags, const float* __restrict__ weight, int n, int V,
-                                                         int32_t* __restrict__ pos, int32_t* __restrict__ rows, int32_t* __restrict__ count) {
+                                                         int32_t* __restrict__ pos, int32_t* __restrict__ rows, int32_t* __restrict__ count, int32_t* __restrict__ redo, int n_redo) {
   __shared__ int wave_sum_s[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < n_redo; i += 1024) redo[i] = 0;
+  const bool vec = ((uintptr_t)targets & 15) == 0 && ((uintptr_t)weight & 15) == 0;
   int base = 0;
   for (int t0 = 0; t0 < n; t0 += 16 * 1024) {
     const int first = t0 + tid * 16;
     uint32_t live = 0;
+    if (flags) {          // flags and pos are 256-byte aligned and padded to 64 rows
+      if (first < n) {
+        const uint4 f = *reinterpret_cast<const uint4*>(flags + first);
+        const uint32_t w[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int t = first + e;
-      if (t < n && (flags ? flags[t] != 0 : hard_row(targets, t, V) && !(weight && weight[t] == 0.f))) live |= 1u << e;
-    }
+        for (int e = 0; e < 16; ++e) live |= ((w[e >> 2] >> (8 * (e & 3)) & 255) != 0 && first + e < n ? 1u : 0u) << e;
+      }
+    } else if (vec && first + 16 <= n) {
+      int4 y[4];
+      float4 g[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        y[q] = *reinterpret_cast<const int4*>(targets + first + 4 * q);
+        g[q] = weight ? *reinterpret_cast<const float4*>(weight + first + 4 * q) : make_float4(1.f, 1.f, 1.f, 1.f);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        auto one = [&](int v, float gv) { return (uint32_t)v < (uint32_t)V && gv != 0.f ? 1u : 0u; };
+        live |= (one(y[q].x, g[q].x) | one(y[q].y, g[q].y) << 1 | one(y[q].z, g[q].z) << 2 | one(y[q].w, g[q].w) << 3) << (4 * q);
+      }
+    } else
+      for (int e = 0; e < 16 && first + e < n; ++e)
+        if (hard_row(targets, first + e, V) && !(weight && weight[first + e] == 0.f)) live |= 1u << e;
     const int mine = __popc(live);
     int incl = mine;
 #pragma unroll
@@ -149,15 +170,20 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
     if (lane == 63) wave_sum_s[wave] = incl;
     __syncthreads();
     int before = base, all = 0;
-    for (int w = 0; w < 16; ++w) { if (w < wave) before += wave_sum_s[w]; all += wave_sum_s[w]; }
-    int at = before + incl - mine;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int t = first + e;
-      if (t >= n) break;
-      const bool l = live >> e & 1;
-      pos[t] = l ? at : -1;
-      if (l) rows[at++] = t;
+    for (int w = 0; w < 16; ++w) { const int v = wave_sum_s[w]; if (w < wave) before += v; all += v; }
+    const int at0 = before + incl - mine;
+    if (first < n) {
+      int at = at0;
+      int pv[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const bool l = live >> e & 1;
+        pv[e] = l ? at : -1;
+        if (l) rows[at++] = first + e;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *reinterpret_cast<int4*>(pos + first + 4 * q) = make_int4(pv[4 * q], pv[4 * q + 1], pv[4 * q + 2], pv[4 * q + 3]);
     }
     base += all;
   }
@@ -194,7 +220,11 @@ template <class T>
 __global__ __launch_bounds__(256) void head_transpose_kernel(const T* __restrict__ src, int ld_src, T* __restrict__ dst, int ld_dst, int rows, int cols) {
   __shared__ T tile[64][65];
   const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  for (int i = ty; i < 64; i += 4) tile[i][tx] = r0 + i < rows && c0 + tx < cols ? src[(size_t)(r0 + i) * ld_src + c0 + tx] : from_f32<T>(0.f);
+  T v[16];          // all rows of a thread requested at once, from clamped addresses
+#pragma unroll
+  for (int k = 0; k < 16; ++k) v[k] = src[(size_t)min(r0 + ty + 4 * k, rows - 1) * ld_src + min(c0 + tx, cols - 1)];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) tile[ty + 4 * k][tx] = r0 + ty + 4 * k < rows ? v[k] : from_f32<T>(0.f);
   __syncthreads();
   for (int i = ty; i < 64; i += 4)
     if (c0 + i < cols && r0 + tx < ld_dst) dst[(size_t)(c0 + i) * ld_dst + r0 + tx] = tile[tx][i];
@@ -293,23 +323,34 @@ __global__ __launch_bounds__(256) void head_row_kernel(const float* z_, T* dz_, 
 }
 
 // ------------------------------------------------------------------------------------------------ bf16: references, sums, losses and the places that differ
-// zsel[i][j] = z of entry j of compact row i (j == top: of its target) by a wave's dot products in fp32, and ref[i] = the largest of them (inf behind the last row that counts).
-// xc and w rows are dp (a multiple of 64) elements, 16-byte aligned.
+// What head_gather_kernel does, and for the rows that count zsel[i][j] = z of entry j of compact row i (j == top: of its target) by a wave's dot products in fp32 and ref[i] = the largest of
+// them (0 behind the last row that counts).  xc and w rows are dp (a multiple of 64) elements, 16-byte aligned.
 struct HeadRef {
-  const bf16_t *xc, *w;
-  int ldw, dp, np, V, top;
-  const int32_t *rows, *count, *targets, *ids;
+  const bf16_t *x, *w;
+  bf16_t *xc, *dx;
+  int ldx, ldw, lddx, d, dp, n, np, V, top, vec;          // vec: rows of x are whole aligned groups of 8
+  const int32_t *pos, *count, *targets, *ids;
   const float* logits;
   const unsigned char* flags;
-  float *zsel, *ref;
+  float *zsel, *ref, *row_loss, *row_lse;
 };
 __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (i >= h.np) return;
-  if (i >= *h.count) { if (lane == 0) h.ref[i] = INFINITY; return; }
-  const int t = h.rows[i];
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (t >= h.np) return;
+  if (t >= *h.count) {
+    for (int c = lane * 8; c < h.dp; c += 512) *reinterpret_cast<uint4*>(h.xc + (size_t)t * h.dp + c) = make_uint4(0, 0, 0, 0);
+    if (lane == 0) h.ref[t] = 0.f;
+  }
+  if (t >= h.n) return;
+  const int i = h.pos[t];
+  if (i < 0) {
+    if (h.dx) for (int c = lane; c < h.d; c += 64) h.dx[(size_t)t * h.lddx + c] = from_f32<bf16_t>(0.f);
+    if (lane == 0) { h.row_loss[t] = 0.f; if (h.row_lse) h.row_lse[t] = 0.f; }
+    return;
+  }
   const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
-  const bf16_t* x = h.xc + (size_t)i * h.dp;
+  const bf16_t* x = h.x + (size_t)t * h.ldx;
+  bf16_t* xc = h.xc + (size_t)i * h.dp;
   float* zs = h.zsel + (size_t)i * (h.top + 1);
   float best = -INFINITY;
   constexpr int NB = 8;          // entries at a time: eight rows of W in flight
@@ -323,9 +364,21 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
       if ((uint32_t)id[e] >= (uint32_t)h.V || (j < h.top && h.logits[(size_t)t * h.top + j] == -INFINITY)) id[e] = -1;
       s[e] = 0.f;
     }
+    const bool copy = j0 + NB > h.top;          // the last round writes the row's copy
     for (int c = lane * 8; c < h.dp; c += 512) {
+      uint4 raw;
+      if (h.vec && c + 8 <= h.d) raw = *reinterpret_cast<const uint4*>(x + c);
+      else {
+        uint16_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + k < h.d ? x[c + k].bits : (uint16_t)0;
+        raw = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
+      }
+      if (copy) *reinterpret_cast<uint4*>(xc + c) = raw;
+      const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
       float xv[8], wv[8];
-      load8(x + c, xv);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { xv[2 * k] = __uint_as_float(rw[k] << 16); xv[2 * k + 1] = __uint_as_float(rw[k] & 0xffff0000u); }
 #pragma unroll
       for (int e = 0; e < NB; ++e)
         if (id[e] >= 0) {
@@ -372,11 +425,28 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
   if (b0 >= live) return;
   const int row = b0 + lane;
   float s1 = 0.f, s2 = 0.f, far = -INFINITY;
-  for (int g = wave; g < h.groups; g += 16) {
-    const float2 v = h.stats[(size_t)g * h.piece + min(row, live - 1)];
+  const float2* sp = h.stats + min(row, live - 1);
+  const float* sp2 = h.stats2 + min(row, live - 1);
+  int g = wave;
+  for (; g + 7 * 16 < h.groups; g += 8 * 16) {          // eight loads in flight
+    float2 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = sp[(size_t)(g + 16 * k) * h.piece];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s1 += v[k].x; far = fmaxf(far, v[k].y); }
+    if (h.mixed) {
+      float u[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) u[k] = sp2[(size_t)(g + 16 * k) * h.piece];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s2 += u[k];
+    }
+  }
+  for (; g < h.groups; g += 16) {
+    const float2 v = sp[(size_t)g * h.piece];
     s1 += v.x;
     far = fmaxf(far, v.y);
-    if (h.mixed) s2 += h.stats2[(size_t)g * h.piece + min(row, live - 1)];
+    if (h.mixed) s2 += sp2[(size_t)g * h.piece];
   }
   s1_s[wave][lane] = s1; s2_s[wave][lane] = s2; top_s[wave][lane] = far;
   __syncthreads();
@@ -555,10 +625,6 @@ __global__ __launch_bounds__(256) void head_et_kernel(const bf16_t* __restrict__
     *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c - v0) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
-__global__ void head_clear_kernel(int32_t* p, int n) {
-  for (int i = threadIdx.x; i < n; i += 256) p[i] = 0;
-}
-
 // ------------------------------------------------------------------------------------------------ outputs
 // dx[rows[i]] = scale[i] sum of the partials [splits][live64][d], a wave per compact row of the piece
 __global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const float* __restrict__ scale, bf16_t* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows,
@@ -606,12 +672,20 @@ __global__ __launch_bounds__(256) void head_add_kernel(const float* __restrict__
     *o = from_f32<TO>(add ? to_f32(*o) + v : v);
   }
 }
-__global__ __launch_bounds__(1024) void head_loss_kernel(const float* __restrict__ row_loss, const float* __restrict__ weight, const int32_t* __restrict__ pos, const int32_t* __restrict__ count,
-                                                         float* __restrict__ loss, int n) {
+// loss = sum of weight * row_loss, or their mean over the rows that count (rows that are left out have a row_loss of 0, and their weight is not looked at)
+__global__ __launch_bounds__(1024) void head_loss_kernel(const float* __restrict__ row_loss, const float* __restrict__ weight, const int32_t* __restrict__ count, float* __restrict__ loss, int n) {
   __shared__ float red[17];
   float s = 0.f;
-  for (int t = threadIdx.x; t < n; t += 1024)
-    if (pos[t] >= 0) s += weight ? weight[t] * row_loss[t] : row_loss[t];
+  auto add = [&](float l, float g) { s += l != 0.f ? g * l : 0.f; };
+  int t = threadIdx.x;
+  for (; t + 7 * 1024 < n; t += 8 * 1024) {          // eight loads in flight
+    float l[8], g[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { l[k] = row_loss[t + 1024 * k]; g[k] = weight ? weight[t + 1024 * k] : 1.f; }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) add(l[k], g[k]);
+  }
+  for (; t < n; t += 1024) add(row_loss[t], weight ? weight[t] : 1.f);
   s = block_sum(s, red);
   if (threadIdx.x == 0) *loss = weight ? s : s / (float)max(*count, 1);
 }
@@ -655,21 +729,21 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
   float *ref = (float*)(ws + p.ref), *scale = (float*)(ws + p.scale), *zsel = (float*)(ws + p.zsel), *part = (float*)(ws + p.part);
   auto* stats = (float2*)(ws + p.stats);
   auto* stats2 = (float*)(ws + p.stats2);
-  auto* redo = (int32_t*)(ws + p.redo);
   auto* coef = p.mixed ? (float2*)(ws + p.coef) : nullptr;
   bf16_t* e = p.grads ? (bf16_t*)(ws + p.z) : nullptr;
   const bf16_t* xc = (const bf16_t*)(ws + p.xc);
   bool ok = true;
-  head_ref_kernel<<<quads(p.np), 256, 0, st>>>(HeadRef{xc, (const bf16_t*)w, ldw, p.dp, p.np, a.vocab, a.top, rows, count, a.targets, a.ids, a.logits, flags, zsel, ref});
+  head_ref_kernel<<<quads(p.np), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
+                                                       a.ldx % 8 == 0 && ((uintptr_t)a.x & 15) == 0, (const int32_t*)(ws + p.pos), count, a.targets, a.ids, a.logits, flags, zsel, ref, row_loss, a.row_lse});
   const float log2e = 1.44269504f;
   for (int i0 = 0; i0 < a.n; i0 += p.piece) {
     const int m = std::min(p.piece, p.np - i0);          // a multiple of 64
     const bf16_t* xp = xc + (size_t)i0 * p.dp;
+    auto* redo = (int32_t*)(ws + p.redo) + (size_t)(i0 / p.piece) * (1 + (p.piece + 255) / 256);
     HeadEpi he{};
     he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp;
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
               !p.mixed, redo, a.tau, a.share};
-    head_clear_kernel<<<1, 256, 0, st>>>(redo, 1 + (m + 255) / 256);
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
     head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
     he.redo = redo;
@@ -731,8 +805,9 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   char* xc = ws + p.xc;
 
   if (a.top && a.n) head_flags_kernel<<<quads(a.n), 256, 0, st>>>(a.targets, a.ids, a.logits, a.row_weight, flags, a.n, a.vocab, a.top, a.share > 0.f);
-  head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count);
-  PP_H_DISPATCH(a.dtype, head_gather_kernel<T><<<quads(p.np), 256, 0, st>>>((const T*)a.x, a.ldx, (T*)xc, p.dp, a.d, pos, count, a.n, p.np, (T*)a.dx, a.lddx, row_loss, a.row_lse));
+  head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count, (int32_t*)(ws + p.redo), p.n_redo);
+  if (a.dtype == 0)
+    head_gather_kernel<float><<<quads(p.np), 256, 0, st>>>((const float*)a.x, a.ldx, (float*)xc, p.dp, a.d, pos, count, a.n, p.np, (float*)a.dx, a.lddx, row_loss, a.row_lse);
   const void* w = a.w;
   int ldw = a.ldw;
   if (p.copy_w) {
@@ -753,7 +828,7 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   bool ok = true;
   if (a.dtype) ok = head_bf16(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
   else head_f32(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
-  if (a.loss) head_loss_kernel<<<1, 1024, 0, st>>>(row_loss, a.row_weight, pos, count, a.loss, a.n);
+  if (a.loss) head_loss_kernel<<<1, 1024, 0, st>>>(row_loss, a.row_weight, count, a.loss, a.n);
   return ok ? 0 : 1;
 }
 

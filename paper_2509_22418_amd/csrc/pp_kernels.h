@@ -144,7 +144,7 @@ struct HeadEpi {
   int i0, piece;
   int rows_are_k;                  // 0: the rows are the product's rows (M = live), 1: its contraction index (K = live)
   // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and 64 columns the sum of e, the largest exponent and, where kt != 0, the sum of
-  // exp2(kt (z - ref)), at [64-column group][row of the piece].  A row with ref = inf gives e = 0.
+  // exp2(kt (z - ref)), at [64-column group][row of the piece].
   const float* ref;
   float2* stats;
   float* stats2;
