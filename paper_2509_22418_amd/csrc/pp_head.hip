@@ -34,7 +34,7 @@ constexpr int kTopMax = 128;          // entries per row (PP_HEAD_TOP_MAX)
 constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
   int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
-  int dx_splits, dw_splits, n_redo;
+  int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
   bool grads, copy_w, own_wt, mixed;
   size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dxc, dwa, dwp, total;          // byte offsets
 };
@@ -52,6 +52,14 @@ int best_splits(long tiles, long steps, double mn) {
   return best;
 }
 
+// Few rows: threads of a workgroup side by side (8 columns each), and rows of W per workgroup such that the workgroups' partial sums of dX are kFewPartials at most.
+constexpr int kFew = 16, kFewPartials = 512;
+int few_cols(int d) { int c = 1; while (c < 256 && c * 8 < d) c *= 2; return c; }
+int few_chunk(int rows, int d) {
+  const int groups = std::max(1, kFewPartials * few_cols(d) / 256);
+  return (rows + groups - 1) / groups;
+}
+
 HeadPlan plan_head(const HeadArgs& a) {
   HeadPlan p{};
   const bool bf = a.dtype != 0;
@@ -63,6 +71,26 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.dp = pad_to(a.d, unit);
   p.vp = pad_to(a.vocab, unit);
   p.np = std::max(64, pad_to(a.n, 64));
+  if (a.n > 0 && a.n <= kFew) {
+    // up to 2048 waves, 8 a compute unit, each with as many of the blocks of 16 rows of W as any other
+    const int tiles = (a.vocab + 15) / 16, each = (tiles + 2047) / 2048;
+    p.parts = ((tiles + each - 1) / each + 3) / 4 * 4;
+    p.vp = pad_to(a.vocab, 16);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
+    p.rowl = take(kFew * 4);
+    p.z = take((size_t)a.n * p.vp * 4);
+    p.stats = take((size_t)kFew * p.parts * 16);
+    p.coef = take(kFew * 16);
+    p.scale = take((size_t)kFew * (a.top + 1) * 4);
+    p.zsel = take((size_t)kFew * (a.top + 1) * 4);
+    if (a.dx) {
+      const int chunk = few_chunk(a.vocab, a.d);
+      p.part = take((size_t)((a.vocab + chunk - 1) / chunk) * (256 / few_cols(a.d)) * a.n * a.d * 4);
+    }
+    p.total = off;
+    return p;
+  }
   p.groups = (a.vocab + 255) / 256 * 4;
   const size_t row = (size_t)p.vp * es;
   p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(kPieceBytes / row / 256 * 256));
@@ -625,6 +653,303 @@ __global__ __launch_bounds__(256) void head_et_kernel(const bf16_t* __restrict__
     *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c - v0) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
+// ------------------------------------------------------------------------------------------------ few rows
+// Up to 16 rows (one block of a 16 x 16 MFMA, whichever storage type): W is streamed once for the losses, by waves that take 16 of its rows at a time from memory straight into
+// MFMA operands, and once for dX; dW is written once.  Bound by those bytes: 32000 x 2048 bf16 (131 MB) at the card's copy rate 25 us.  Logits in fp32 (16 rows of them at most),
+// dz in fp32 and not rounded.  Fixed orders throughout: no atomics.
+struct HeadFew {
+  const void *x, *w;
+  int ldx, ldw, n, V, d, ldz, parts, top, dw_lo, dw_hi, lddx, lddw, dw_add, chunk, vec;          // parts: waves of the first kernel; chunk: rows of W per workgroup of the others
+  const int32_t *targets, *ids;
+  const float *logits, *weight;
+  float tau, share;
+  float *z, *part, *coef, *sub, *psum;          // z [n][ldz], part [16][parts][4], coef [16][4], sub [16][top + 1], psum [partials][n][d]
+  int32_t *sid;                                 // [16][top + 1]: where sub is taken off, -1: nowhere
+  float *loss, *row_loss, *row_lse;
+  void *dx, *dw;
+};
+typedef float few_f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 few_bf16x8 __attribute__((ext_vector_type(8)));
+template <class T> struct FewChunk;          // 16 bytes of a row: 8 bf16 or 4 floats
+template <> struct FewChunk<bf16_t> { static constexpr int E = 8; };
+template <> struct FewChunk<float> { static constexpr int E = 4; };
+
+template <class T, bool VEC> __device__ __forceinline__ uint4 few_load(const T* row, int k, int d) {          // elements k .. of a row, zeros from d on
+  constexpr int E = FewChunk<T>::E;
+  if (VEC && k + E <= d) return *reinterpret_cast<const uint4*>(row + k);
+  union { uint4 u; T e[E]; } r;
+#pragma unroll
+  for (int i = 0; i < E; ++i) r.e[i] = k + i < d ? row[k + i] : from_f32<T>(0.f);
+  return r.u;
+}
+__device__ __forceinline__ void few_mfma(few_f32x4& acc, const uint4& a, const uint4& b, bf16_t) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(few_bf16x8, a), __builtin_bit_cast(few_bf16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void few_mfma(few_f32x4& acc, const uint4& a, const uint4& b, float) {          // the four k of a lane's chunk, one per MFMA
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+}
+// (m, s) of a softmax's maximum and sum, s2 the sum at the teacher's temperature
+__device__ __forceinline__ void few_merge(float& m, float& s, float& s2, float mo, float so, float so2, float it) {
+  const float top = fmaxf(m, mo);
+  if (top == -INFINITY) { s += so; s2 += so2; return; }          // nothing yet on either side (or only NaN, which both keep)
+  const float a = expf(m - top), b = expf(mo - top);
+  s = s * a + so * b;
+  s2 = it == 1.f ? s : s2 * expf((m - top) * it) + so2 * expf((mo - top) * it);
+  m = top;
+}
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void head_few_z_kernel(HeadFew h) {
+  constexpr int E = FewChunk<T>::E, U = 8, STEP = 4 * E;          // k per MFMA step of the four lane groups
+  const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4, gw = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const T* x = (const T*)h.x + (size_t)min(l16, h.n - 1) * h.ldx;
+  const float it = 1.0f / h.tau;
+  float m = -INFINITY, s = 0.f, s2 = 0.f;
+  for (int tile = gw; tile * 16 < h.V; tile += h.parts) {
+    const T* w = (const T*)h.w + (size_t)min(tile * 16 + l16, h.V - 1) * h.ldw;
+    few_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    uint4 a[2][U], b[2][U];
+    auto fetch = [&](int buf, int k0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) a[buf][u] = few_load<T, VEC>(w, k0 + u * STEP + lq * E, h.d);
+#pragma unroll
+      for (int u = 0; u < U; ++u) b[buf][u] = few_load<T, VEC>(x, k0 + u * STEP + lq * E, h.d);
+    };
+    auto multiply = [&](int buf) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) few_mfma(acc, a[buf][u], b[buf][u], T{});
+    };
+    fetch(0, 0);
+    for (int k0 = 0; k0 < h.d; k0 += 2 * U * STEP) {          // chunks behind d are zeros without a load
+      fetch(1, k0 + U * STEP);
+      multiply(0);
+      fetch(0, k0 + 2 * U * STEP);
+      multiply(1);
+    }
+    // element r: row 4 lq + r of the 16 rows of W, token l16
+    const int v0 = tile * 16 + 4 * lq;
+    if (l16 < h.n) *reinterpret_cast<float4*>(h.z + (size_t)l16 * h.ldz + v0) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    float tm = -INFINITY, ts = 0.f, ts2 = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (v0 + r >= h.V) acc[r] = -INFINITY;
+      tm = fmaxf(tm, acc[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (acc[r] != -INFINITY) { ts += expf(acc[r] - tm); if (it != 1.f) ts2 += expf((acc[r] - tm) * it); }
+    few_merge(m, s, s2, tm, ts, it == 1.f ? ts : ts2, it);
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) few_merge(m, s, s2, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(s2, o, 64), it);
+  if (lq == 0) *reinterpret_cast<float4*>(h.part + ((size_t)l16 * h.parts + gw) * 4) = make_float4(m, s, s2, 0.f);
+}
+
+// One block, a wave per row: losses, and for the gradients dz = coef[1] exp(z - coef[0]) + coef[2] exp((z - coef[0]) / tau) - sub at sid (all 0 for a row that is left out)
+__global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
+  __shared__ int live_s[kFew], id_s[kFew][kTopMax];
+  __shared__ float loss_s[kFew], q_s[kFew][kTopMax];
+  const int lane = threadIdx.x & 63, t = threadIdx.x >> 6;
+  const float it = 1.0f / h.tau, w = t < h.n && h.weight ? h.weight[t] : 1.f;
+  int id[2] = {-1, -1};
+  float u[2] = {-INFINITY, -INFINITY}, q[2] = {0.f, 0.f};
+  bool hard = false, soft = false;
+  float l = 0.f, lse = 0.f, m = -INFINITY, s = 0.f, s2 = 0.f;
+  if (t < h.n) {
+    hard = w != 0.f && hard_row(h.targets, t, h.V);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int j = lane + 64 * k;
+      if (j < h.top && h.share > 0.f && w != 0.f) {
+        id[k] = h.ids[(size_t)t * h.top + j];
+        if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j] * it; else id[k] = -1;
+        if (u[k] == -INFINITY) id[k] = -1;
+      }
+    }
+    soft = __ballot(id[0] >= 0 || id[1] >= 0) != 0;
+    for (int g = lane; g < h.parts; g += 64) {
+      const float4 p = *reinterpret_cast<const float4*>(h.part + ((size_t)t * h.parts + g) * 4);
+      few_merge(m, s, s2, p.x, p.y, p.z, it);
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) few_merge(m, s, s2, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(s2, o, 64), it);
+  }
+  if (lane == 0) live_s[t] = hard || soft;
+  __syncthreads();
+  int count = 0;
+  for (int k = 0; k < kFew; ++k) count += live_s[k];
+  const bool live = hard || soft;
+  const float* z = h.z + (size_t)min(t, h.n - 1) * h.ldz;
+  const int y = hard ? h.targets[t] : -1;
+  const float zy = hard ? z[y] : 0.f;
+  float zj[2] = {0.f, 0.f};
+  if (soft) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (id[k] >= 0) zj[k] = z[id[k]];
+    const float um = wave_max(fmaxf(id[0] >= 0 ? u[0] : -INFINITY, id[1] >= 0 ? u[1] : -INFINITY));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf(u[k] - um) : 0.f;
+    const float sum = wave_sum(q[0] + q[1]), lst = logf(s2);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      q[k] /= sum;
+      if (id[k] >= 0 && !(q[k] <= 0.f)) l += q[k] * (logf(q[k]) - (zj[k] - m) * it + lst);
+    }
+    l = wave_sum(l) * h.share * h.tau * h.tau;
+  }
+  if (hard) l += (1.f - h.share) * ((m - zy) + logf(s));
+  if (live) lse = m * it + logf(s2);
+  const float g = h.weight ? w : 1.0f / (float)max(count, 1);
+  if (t < h.n && lane == 0) { h.row_loss[t] = l; if (h.row_lse) h.row_lse[t] = lse; }
+  if (lane == 0) loss_s[t] = live ? (h.weight ? w * l : l) : 0.f;
+  // gradients' coefficients
+  const float c1 = hard ? g * (1.f - h.share) : 0.f, ct = soft ? g * h.share * h.tau : 0.f;
+  if (lane == 0) *reinterpret_cast<float4*>(h.coef + t * 4) = make_float4(m, hard ? c1 / s : 0.f, soft ? ct / s2 : 0.f, live ? 1.f : 0.f);
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    if (lane + 64 * k < h.top) { id_s[t][lane + 64 * k] = id[k]; q_s[t][lane + 64 * k] = q[k]; }
+  __syncthreads();
+  bool y_listed = false;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int j = lane + 64 * k;
+    if (j >= h.top) continue;
+    bool first = id[k] >= 0;
+    float sub = id[k] == y ? c1 : 0.f;
+    y_listed |= hard && id[k] == y;
+    if (id[k] >= 0)
+      for (int o = 0; o < h.top; ++o)
+        if (id_s[t][o] == id[k]) { if (o < j) first = false; sub += ct * q_s[t][o]; }
+    h.sid[t * (h.top + 1) + j] = first ? id[k] : -1;
+    h.sub[t * (h.top + 1) + j] = sub;
+  }
+  const bool listed = __ballot(y_listed) != 0;
+  if (lane == 0) { h.sid[t * (h.top + 1) + h.top] = hard && !listed ? y : -1; h.sub[t * (h.top + 1) + h.top] = c1; }
+  if (threadIdx.x == 0 && h.loss) {
+    float a = 0.f;
+    for (int k = 0; k < kFew; ++k) a += loss_s[k];
+    *h.loss = h.weight ? a : a / (float)max(count, 1);
+  }
+}
+
+// dz of rows v0 .. v0 + rows - 1 of W for NT tokens into shared memory; every thread calls it
+template <int NT>
+__device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float (*dz)[128]) {
+  const float it = 1.0f / h.tau;
+  __syncthreads();
+  for (int i = threadIdx.x; i < NT * 128; i += 256) {
+    const int t = i >> 7, r = i & 127;
+    float v = 0.f;
+    if (t < h.n && r < rows) {
+      const float4 c = *reinterpret_cast<const float4*>(h.coef + t * 4);
+      const float a = h.z[(size_t)t * h.ldz + v0 + r] - c.x;
+      if (c.w != 0.f) v = (c.y != 0.f ? c.y * expf(a) : 0.f) + (c.z != 0.f ? c.z * expf(a * it) : 0.f);
+    }
+    dz[t][r] = v;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < h.n * (h.top + 1); i += 256) {          // no two entries of a row have the same place
+    const int t = i / (h.top + 1), v = h.sid[i];
+    if (v >= v0 && v < v0 + rows) dz[t][v - v0] -= h.sub[i];
+  }
+  __syncthreads();
+}
+// Threads of a workgroup: `cols` of them side by side, 8 columns each, 256 / cols rows of W at a time
+template <class T, int NT>
+__global__ __launch_bounds__(256) void head_few_dx_kernel(HeadFew h, int cols) {
+  __shared__ float dz[NT][128];
+  const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
+  const int lo = blockIdx.x * h.chunk, hi = min(lo + h.chunk, h.V);
+  float acc[NT][8];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[t][e] = 0.f;
+  const T* w = (const T*)h.w;
+  for (int v0 = lo; v0 < hi; v0 += 128) {
+    const int rows = min(128, hi - v0);
+    few_dz<NT>(h, v0, rows, dz);
+    if (c >= h.d) continue;          // uniform barriers: few_dz is reached by every thread at every trip
+    auto row = [&](int r) {
+      float v[8];
+      const T* p = w + (size_t)(v0 + r) * h.ldw + c;
+      if (h.vec && c + 8 <= h.d) load8(p, v);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < h.d ? to_f32(p[e]) : 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float g = dz[t][r];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[t][e] = fmaf(g, v[e], acc[t][e]);
+      }
+    };
+    int r = rg;
+    for (; r + 3 * rp < rows; r += 4 * rp) { row(r); row(r + rp); row(r + 2 * rp); row(r + 3 * rp); }
+    for (; r < rows; r += rp) row(r);
+  }
+  if (c >= h.d) return;
+  float* out = h.psum + (size_t)(blockIdx.x * rp + rg) * h.n * h.d;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    if (t < h.n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < h.d) out[(size_t)t * h.d + c + e] = acc[t][e];
+}
+// dx = sum of the partials, a block per row and 64 columns, 16 waves of partials
+template <class T>
+__global__ __launch_bounds__(1024) void head_few_sum_kernel(HeadFew h, int partials) {
+  __shared__ float s_s[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = blockIdx.y, c = blockIdx.x * 64 + lane;
+  float s = 0.f;
+  if (c < h.d)
+    for (int p = wave; p < partials; p += 16) s += h.psum[((size_t)p * h.n + t) * h.d + c];
+  s_s[wave][lane] = s;
+  __syncthreads();
+  if (wave || c >= h.d) return;
+  for (int k = 1; k < 16; ++k) s += s_s[k][lane];
+  ((T*)h.dx)[(size_t)t * h.lddx + c] = from_f32<T>(h.coef[t * 4 + 3] != 0.f ? s : 0.f);
+}
+template <class T, class TO, int NT>
+__global__ __launch_bounds__(256) void head_few_dw_kernel(HeadFew h, int cols) {
+  __shared__ float dz[NT][128];
+  const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
+  const int lo = h.dw_lo + blockIdx.x * h.chunk, hi = min(lo + h.chunk, h.dw_hi);
+  float x[NT][8];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[t][e] = t < h.n && c + e < h.d && h.coef[t * 4 + 3] != 0.f ? to_f32(((const T*)h.x)[(size_t)t * h.ldx + c + e]) : 0.f;
+  for (int v0 = lo; v0 < hi; v0 += 128) {
+    const int rows = min(128, hi - v0);
+    few_dz<NT>(h, v0, rows, dz);
+    if (c >= h.d) continue;
+    for (int r = rg; r < rows; r += rp) {
+      float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float g = dz[t][r];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(g, x[t][e], o[e]);
+      }
+      TO* p = (TO*)h.dw + (size_t)(v0 + r - h.dw_lo) * h.lddw + c;
+      const bool whole = c + 8 <= h.d && h.lddw % 8 == 0 && ((uintptr_t)h.dw & 15) == 0;
+      if (h.dw_add)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (c + e < h.d) o[e] += to_f32(p[e]);
+      if (whole) store8(p, o);
+      else
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (c + e < h.d) p[e] = from_f32<TO>(o[e]);
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ outputs
 // dx[rows[i]] = scale[i] sum of the partials [splits][live64][d], a wave per compact row of the piece
 __global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const float* __restrict__ scale, bf16_t* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows,
@@ -692,6 +1017,38 @@ __global__ __launch_bounds__(1024) void head_loss_kernel(const float* __restrict
 
 // ------------------------------------------------------------------------------------------------ one call
 static dim3 quads(int rows) { return dim3((rows + 3) / 4); }
+
+template <class T, int NT>
+static void few_grads(hipStream_t st, const HeadArgs& a, HeadFew h) {
+  const int cols = few_cols(a.d), slices = (a.d + cols * 8 - 1) / (cols * 8);
+  if (a.dx) {
+    h.chunk = few_chunk(a.vocab, a.d);
+    const int groups = (a.vocab + h.chunk - 1) / h.chunk;
+    head_few_dx_kernel<T, NT><<<dim3(groups, slices), 256, 0, st>>>(h, cols);
+    head_few_sum_kernel<T><<<dim3((a.d + 63) / 64, a.n), 1024, 0, st>>>(h, groups * (256 / cols));
+  }
+  if (a.dw) {
+    const int rows = a.dw_hi - a.dw_lo;
+    h.chunk = std::max(1, std::min(128, (rows * slices + 1023) / 1024));
+    const dim3 grid((rows + h.chunk - 1) / h.chunk, slices);
+    if (a.dw_f32) head_few_dw_kernel<T, float, NT><<<grid, 256, 0, st>>>(h, cols);
+    else head_few_dw_kernel<T, T, NT><<<grid, 256, 0, st>>>(h, cols);
+  }
+}
+template <class T>
+static void head_few(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, float* row_loss) {
+  HeadFew h{a.x, a.w, a.ldx, a.ldw, a.n, a.vocab, a.d, p.vp, p.parts, a.top, a.dw_lo, a.dw_hi, a.lddx, a.lddw, a.dw_f32 == 2, 0, 0, a.targets, a.ids, a.logits, a.row_weight, a.tau, a.share,
+            (float*)(ws + p.z), (float*)(ws + p.stats), (float*)(ws + p.coef), (float*)(ws + p.scale), (float*)(ws + p.part), (int32_t*)(ws + p.zsel), a.loss, row_loss, a.row_lse, a.dx, a.dw};
+  constexpr int E = FewChunk<T>::E;
+  h.vec = a.ldw % 8 == 0 && ((uintptr_t)a.w & 15) == 0;
+  const bool vec = a.ldw % E == 0 && a.ldx % E == 0 && (((uintptr_t)a.w | (uintptr_t)a.x) & 15) == 0;
+  if (vec) head_few_z_kernel<T, true><<<p.parts / 4, 256, 0, st>>>(h);
+  else head_few_z_kernel<T, false><<<p.parts / 4, 256, 0, st>>>(h);
+  head_few_fin_kernel<<<1, 1024, 0, st>>>(h);
+  if (a.n == 1) few_grads<T, 1>(st, a, h);
+  else if (a.n <= 4) few_grads<T, 4>(st, a, h);
+  else few_grads<T, 16>(st, a, h);
+}
 
 static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, const void* w, int ldw, const void* wt, int ldwt, float* row_loss) {
   const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
@@ -804,6 +1161,10 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   float* row_loss = a.row_loss ? a.row_loss : (float*)(ws + p.rowl);
   char* xc = ws + p.xc;
 
+  if (p.parts) {
+    PP_H_DISPATCH(a.dtype, head_few<T>(st, a, p, ws, row_loss));
+    return 0;
+  }
   if (a.top && a.n) head_flags_kernel<<<quads(a.n), 256, 0, st>>>(a.targets, a.ids, a.logits, a.row_weight, flags, a.n, a.vocab, a.top, a.share > 0.f);
   head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count, (int32_t*)(ws + p.redo), p.n_redo);
   if (a.dtype == 0)
