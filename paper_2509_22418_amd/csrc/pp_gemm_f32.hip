@@ -57,6 +57,9 @@ struct F32GemmArgs {
   int lda, ldb, ldc, M, N, K, kchunk;
   int m_blk; long a_blk_stride;          // TN only: column m of the product is column (m / m_blk) * a_blk_stride + m % m_blk of A
   int epi;
+  // Rows that count, where only the device knows their number (nullptr: all): live = clamp(*count - i0, 0, piece).  NT: tiles of rows behind them are not formed (nor written); TN: the
+  // contraction ends with them.
+  const int32_t* count; int i0, piece;
 };
 
 // VEC: groups of four elements are aligned and exist as a whole
@@ -71,7 +74,9 @@ __global__ __launch_bounds__(256) void gemm_f32_mfma_kernel(const T* __restrict_
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int lr = SMALL ? lane & 15 : lane & 31, lg = SMALL ? lane >> 4 : lane >> 5;          // row within a wave's block, k group of the MFMA
   const int m0 = blockIdx.y * BM, n0 = blockIdx.x * BM, z = blockIdx.z;
-  const int kb = z * g.kchunk, ke = min(g.K, kb + g.kchunk), nk = (ke - kb + BK - 1) / BK;
+  const int live = g.count ? min(max(*g.count - g.i0, 0), g.piece) : 0x7fffffff;
+  if (!TN && m0 >= live) return;
+  const int kb = z * g.kchunk, ke = TN ? max(kb, min(min(g.K, live), kb + g.kchunk)) : min(g.K, kb + g.kchunk), nk = (ke - kb + BK - 1) / BK;
   // float offset of chunk c of row r in an NT panel
   auto at = [](int r, int c) {
     if constexpr (SMALL) return (r * CPR + (c ^ (((r & 1) << 1) | ((r >> 1) & 1) | (r & 12)))) * 4;
@@ -313,14 +318,14 @@ static bool offsets_fit(int lda, int ldb, int K) { return (64ull * (size_t)(lda 
 static bool vec4_ok(int dtype, const void* p, int ld) { return ld % 4 == 0 && ((uintptr_t)p & (dtype == 0 ? 15 : 7)) == 0; }
 
 void k_gemm_nt_f32(hipStream_t st, int dtype, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int epi, const void* R,
-                   int out_f32, int splits, float* partial) {
+                   int out_f32, int splits, float* partial, const int32_t* count, int i0, int piece) {
   if (M == 0 || N == 0) return;
   if (!offsets_fit(lda, ldb, K)) {
     if (splits > 1) k_gemm_nt_plain_splitk(st, dtype, A, lda, B, ldb, partial, M, N, K, splits);
     else k_gemm_nt_plain(st, dtype, A, lda, B, ldb, C, ldc, M, N, K, epi, R, out_f32);
     return;
   }
-  const F32GemmArgs g{lda, ldb, splits > 1 ? N : ldc, M, N, K, K / splits, M, 0, epi};
+  const F32GemmArgs g{lda, ldb, splits > 1 ? N : ldc, M, N, K, K / splits, M, 0, epi, count, i0, piece};
   const bool vec = vec4_ok(dtype, A, lda) && vec4_ok(dtype, B, ldb) && g.kchunk % 4 == 0;
   void* out = splits > 1 ? (void*)partial : C;
   if (dtype == 0) launch_f32<float, float, false>(st, A, B, out, R, g, splits, vec);
@@ -330,10 +335,10 @@ void k_gemm_nt_f32(hipStream_t st, int dtype, const void* A, int lda, const void
 
 // returns 1 (nothing launched) if a group of four columns of A could straddle two column blocks, or rows are too long for the offsets
 int k_gemm_tn_f32(hipStream_t st, const float* A, int lda, int m_blk, long a_blk_stride, const float* B, int ldb, float* C, int ldc, int M, int N, int K,
-                  int splits, float* partial) {
+                  int splits, float* partial, const int32_t* count, int i0, int piece) {
   if ((M > m_blk && (m_blk % 4 || a_blk_stride % 4)) || !offsets_fit(lda, ldb, 0)) return 1;
   if (M == 0 || N == 0) return 0;
-  const F32GemmArgs g{lda, ldb, splits > 1 ? N : ldc, M, N, K, K / splits, m_blk, a_blk_stride, EPI_STORE};
+  const F32GemmArgs g{lda, ldb, splits > 1 ? N : ldc, M, N, K, K / splits, m_blk, a_blk_stride, EPI_STORE, count, i0, piece};
   const bool vec = vec4_ok(0, A, lda) && vec4_ok(0, B, ldb) && M % 4 == 0 && N % 4 == 0;
   launch_f32<float, float, true>(st, A, B, splits > 1 ? partial : C, nullptr, g, splits, vec);
   return 0;

@@ -36,7 +36,7 @@ struct HeadPlan {
   int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
   int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
   bool grads, copy_w, own_wt, mixed;
-  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dxc, dwa, dwp, total;          // byte offsets
+  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dwa, total;          // byte offsets
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
@@ -64,11 +64,11 @@ HeadPlan plan_head(const HeadArgs& a) {
   HeadPlan p{};
   const bool bf = a.dtype != 0;
   const size_t es = bf ? 2 : 4;
-  const int unit = bf ? 64 : 4;
+  const int unit = bf ? 64 : 128;          // fp32: dX's contraction in up to 32 ranges of whole groups of four
   const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
   p.grads = a.dx || a.dw;
   p.mixed = a.tau != 1.f && a.share > 0.f && a.share < 1.f;
-  p.dp = pad_to(a.d, unit);
+  p.dp = pad_to(a.d, bf ? 64 : 4);
   p.vp = pad_to(a.vocab, unit);
   p.np = std::max(64, pad_to(a.n, 64));
   if (a.n > 0 && a.n <= kFew) {
@@ -126,10 +126,13 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.part = take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
     p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
   } else {
+    // ranges of the contractions: doubled until the products have two workgroups of 32 x 32 tiles for a compute unit
+    auto double_up = [](long tiles, int k, int unit_k) { int s = 1; while (s < 32 && tiles * s < 512 && k % (2 * s * unit_k) == 0 && k / (2 * s) >= 256) s *= 2; return s; };
+    const long t32 = (a.d + 31) / 32;
+    p.dx_splits = a.dx ? double_up((p.piece + 31) / 32 * t32, p.vp, 4) : 1;
+    p.dw_splits = a.dw ? double_up((dw_rows + 31) / 32 * t32, p.piece, 4) : 1;
     p.z = take((size_t)p.piece * p.vp * 4);
-    p.dxc = take(a.dx ? (size_t)p.piece * p.dp * es : 0);
-    p.dwa = take((size_t)dw_rows * a.d * 4);
-    p.dwp = take(p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
+    p.part = take(std::max(a.dx ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 || p.piece < a.n || a.dw_f32 == 2 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
   }
   p.total = off;
   return p;
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(256) void head_transpose_kernel(const T* __restrict
 }
 
 // ------------------------------------------------------------------------------------------------ softmax, losses and dz of a row of logits
-// One block per compact row of the piece.  z [piece x vp] fp32; dz [piece x vp] in storage type (may be z itself) or nullptr.  Rows from *count on get zeros.
+// One block per compact row of the piece: z [piece x vp] fp32 becomes dz (columns behind the vocabulary zero) if `grads`.
 struct HeadRow {
   const int32_t *rows, *count, *targets, *ids;
   const float *logits, *weight;
@@ -286,50 +289,65 @@ __device__ __forceinline__ void head_entries(const HeadRow& h, int t, int* id_s,
   __syncthreads();
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void head_row_kernel(const float* z_, T* dz_, HeadRow h) {
+// BS threads, NV groups of four logits a thread held in registers (0: the row is read again for each pass).  One read and one write of the row where it fits.
+template <int BS, int NV>
+__global__ __launch_bounds__(BS) void head_row_kernel(float* z_, int grads, HeadRow h) {
   __shared__ float red[17];
   __shared__ int id_s[kTopMax];
   __shared__ float q_s[kTopMax];
   const int i = h.i0 + blockIdx.x, tid = threadIdx.x, n_live = *h.count;
-  const float* z = z_ + (size_t)blockIdx.x * h.vp;
-  T* dz = dz_ ? dz_ + (size_t)blockIdx.x * h.vp : nullptr;
-  if (i >= n_live) {
-    if (dz) for (int v = tid; v < h.vp; v += 256) dz[v] = from_f32<T>(0.f);
-    return;
-  }
-  const int t = h.rows[i];
+  if (i >= n_live) return;          // nothing reads these rows
+  float* z = z_ + (size_t)blockIdx.x * h.vp;
+  const int t = h.rows[i], groups = h.vp / 4;
   const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
   const float it = 1.0f / h.tau;
+  constexpr int KEEP = NV > 0 ? NV : 1;
+  float4 r[KEEP];
+  auto fetch = [&](int g) {          // columns behind the vocabulary as -inf
+    float4 v = g < groups ? *reinterpret_cast<const float4*>(z + 4 * g) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (4 * g + 4 > h.V) { if (4 * g >= h.V) v.x = -INFINITY; if (4 * g + 1 >= h.V) v.y = -INFINITY; if (4 * g + 2 >= h.V) v.z = -INFINITY; v.w = -INFINITY; }
+    return v;
+  };
+  auto each = [&](auto f) {          // f(group index, its four logits)
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) f(tid + BS * k, r[k]);
+    } else
+      for (int g = tid; g < groups; g += BS) f(g, fetch(g));
+  };
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) r[k] = fetch(tid + BS * k);
+  }
   float m = -INFINITY;
-  for (int v = tid; v < h.V; v += 256) m = fmaxf(m, z[v]);
+  each([&](int, const float4& v) { m = fmaxf(fmaxf(m, fmaxf(v.x, v.y)), fmaxf(v.z, v.w)); });
   m = block_max(m, red);
   float s1 = 0.f, st = 0.f;
-  for (int v = tid; v < h.V; v += 256) {
-    s1 += expf(z[v] - m);
-    if (h.tau != 1.f) st += expf((z[v] - m) * it);
-  }
+  const bool two = h.tau != 1.f;
+  each([&](int, const float4& v) {
+    s1 += expf(v.x - m) + expf(v.y - m) + expf(v.z - m) + expf(v.w - m);
+    if (two) st += expf((v.x - m) * it) + expf((v.y - m) * it) + expf((v.z - m) * it) + expf((v.w - m) * it);
+  });
   s1 = block_sum(s1, red);
-  st = h.tau != 1.f ? block_sum(st, red) : s1;
+  st = two ? block_sum(st, red) : s1;
   if (soft) head_entries(h, t, id_s, q_s, red);
   const int y = hard ? h.targets[t] : -1;
   // losses
   float kl = 0.f;
   if (soft && tid < h.top && id_s[tid] >= 0 && !(q_s[tid] <= 0.f)) kl = q_s[tid] * (logf(q_s[tid]) - (z[id_s[tid]] - m) * it + logf(st));
-  kl = block_sum(kl, red);
+  if (h.top) kl = block_sum(kl, red);
   if (tid == 0) {
     float l = soft ? h.share * h.tau * h.tau * kl : 0.f;
     if (hard) l += (1.f - h.share) * ((m - z[y]) + logf(s1));
     h.row_loss[t] = l;
     if (h.row_lse) h.row_lse[t] = m * it + logf(st);
   }
-  if (!dz) return;
-  const float g = h.weight ? h.weight[t] : 1.0f / (float)max(n_live, 1);
+  if (!grads) return;
+  const float g = h.weight ? h.weight[t] : 1.0f / (float)n_live;
   const float c1 = hard ? g * (1.f - h.share) : 0.f, ct = soft ? g * h.share * h.tau : 0.f;
   const float p1 = c1 / s1, pt = ct / st;
   auto soft_part = [&](float zv) { return (c1 != 0.f ? p1 * expf(zv - m) : 0.f) + (ct != 0.f ? pt * expf((zv - m) * it) : 0.f); };
-  // entry j of the row, or the target (j == top): its part of dz is formed from z before the row may be overwritten (dz may be z).  The first of equal
-  // ids stores the sum of all, in their order.
+  // entry j of the row, or the target (j == top): its part of dz is formed from z before dz takes its place.  The first of equal ids stores the sum of all, in their order.
   float own = 0.f;
   int at = -1;
   if (tid <= h.top) {
@@ -345,9 +363,9 @@ __global__ __launch_bounds__(256) void head_row_kernel(const float* z_, T* dz_, 
     }
   }
   __syncthreads();
-  for (int v = tid; v < h.vp; v += 256) dz[v] = from_f32<T>(v < h.V ? soft_part(z[v]) : 0.f);
+  each([&](int gi, const float4& v) { if (gi < groups) *reinterpret_cast<float4*>(z + 4 * gi) = make_float4(soft_part(v.x), soft_part(v.y), soft_part(v.z), soft_part(v.w)); });
   __syncthreads();
-  if (at >= 0) dz[at] = from_f32<T>(own);
+  if (at >= 0) z[at] = own;
 }
 
 // ------------------------------------------------------------------------------------------------ bf16: references, sums, losses and the places that differ
@@ -362,16 +380,18 @@ struct HeadRef {
   const unsigned char* flags;
   float *zsel, *ref, *row_loss, *row_lse;
 };
+constexpr int kRefGroup = 16;
 __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= h.np) return;
-  if (t >= *h.count) {
+  if (t >= *h.count && blockIdx.y == 0) {
     for (int c = lane * 8; c < h.dp; c += 512) *reinterpret_cast<uint4*>(h.xc + (size_t)t * h.dp + c) = make_uint4(0, 0, 0, 0);
     if (lane == 0) h.ref[t] = 0.f;
   }
   if (t >= h.n) return;
   const int i = h.pos[t];
   if (i < 0) {
+    if (blockIdx.y) return;
     if (h.dx) for (int c = lane; c < h.d; c += 64) h.dx[(size_t)t * h.lddx + c] = from_f32<bf16_t>(0.f);
     if (lane == 0) { h.row_loss[t] = 0.f; if (h.row_lse) h.row_lse[t] = 0.f; }
     return;
@@ -381,18 +401,22 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   bf16_t* xc = h.xc + (size_t)i * h.dp;
   float* zs = h.zsel + (size_t)i * (h.top + 1);
   float best = -INFINITY;
+  // Entries in groups of kRefGroup over blockIdx.y, the target (entry `top`) and the row's copy with the first; the reference is the largest of that first group.
   constexpr int NB = 8;          // entries at a time: eight rows of W in flight
-  for (int j0 = soft ? 0 : h.top; j0 <= h.top; j0 += NB) {
+  const int lo = blockIdx.y * kRefGroup, hi = soft ? min(lo + kRefGroup, h.top) : lo;
+  if (blockIdx.y && lo >= hi) return;
+  const int list = hi - lo + (blockIdx.y == 0);          // entries of this wave, the target last
+  for (int k0 = 0; k0 < list; k0 += NB) {
     int id[NB];
     float s[NB];
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
-      const int j = j0 + e;
-      id[e] = j < h.top ? h.ids[(size_t)t * h.top + j] : j == h.top && hard ? h.targets[t] : -1;
-      if ((uint32_t)id[e] >= (uint32_t)h.V || (j < h.top && h.logits[(size_t)t * h.top + j] == -INFINITY)) id[e] = -1;
+      const int j = lo + k0 + e;
+      id[e] = j < hi ? h.ids[(size_t)t * h.top + j] : j == hi && blockIdx.y == 0 && hard ? h.targets[t] : -1;
+      if ((uint32_t)id[e] >= (uint32_t)h.V || (j < hi && h.logits[(size_t)t * h.top + j] == -INFINITY)) id[e] = -1;
       s[e] = 0.f;
     }
-    const bool copy = j0 + NB > h.top;          // the last round writes the row's copy
+    const bool copy = blockIdx.y == 0 && k0 == 0;
     for (int c = lane * 8; c < h.dp; c += 512) {
       uint4 raw;
       if (h.vec && c + 8 <= h.d) raw = *reinterpret_cast<const uint4*>(x + c);
@@ -419,14 +443,14 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
     for (int e = 0; e < NB; ++e)
       if (id[e] >= 0) {
         const float z = wave_sum(s[e]);
-        if (lane == 0) zs[j0 + e] = z;
+        if (lane == 0) zs[lo + k0 + e == hi ? h.top : lo + k0 + e] = z;
         best = fmaxf(best, z);
       }
   }
-  if (lane == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
+  if (lane == 0 && blockIdx.y == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
 }
 
-// A block per 64 compact rows of the piece: sums over the 64-column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
+// A block per 16 compact rows of the piece: sums over the 64-column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
 // entries.  `again`: only rows of blocks that were done again.
 struct HeadFin {
   const float2* stats;
@@ -444,58 +468,58 @@ struct HeadFin {
 };
 constexpr float kFar = 40.f;          // e <= exp(40): sums of 2^20 of them, times what dX's product adds up, stay far from overflow, and C far from underflow
 __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
-  __shared__ float s1_s[16][64], s2_s[16][64], top_s[16][64];
-  __shared__ int id_s[16][kTopMax + 1];
-  __shared__ float q_s[16][kTopMax + 1];
+  __shared__ float s1_s[64][17], s2_s[64][17], top_s[64][17];          // 17: columns on different banks
+  __shared__ __align__(16) int id_s[16][kTopMax];
+  __shared__ float q_s[16][kTopMax];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b0 = blockIdx.x * 64, live = min(max(*h.count - h.i0, 0), h.piece);
+  const int b0 = blockIdx.x * 16, live = min(max(*h.count - h.i0, 0), h.piece);
   if (h.again) { if (!h.redo[0] || !h.redo[1 + b0 / 256]) return; }
   if (b0 >= live) return;
-  const int row = b0 + lane;
-  float s1 = 0.f, s2 = 0.f, far = -INFINITY;
-  const float2* sp = h.stats + min(row, live - 1);
-  const float* sp2 = h.stats2 + min(row, live - 1);
-  int g = wave;
-  for (; g + 7 * 16 < h.groups; g += 8 * 16) {          // eight loads in flight
-    float2 v[8];
+  {
+    const int row = min(b0 + (tid & 15), live - 1), slice = tid >> 4;
+    float s1 = 0.f, s2 = 0.f, far = -INFINITY;
+    const float2* sp = h.stats + row;
+    const float* sp2 = h.stats2 + row;
+    int g = slice;
+    for (; g + 7 * 64 < h.groups; g += 8 * 64) {          // eight loads in flight
+      float2 v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = sp[(size_t)(g + 16 * k) * h.piece];
+      for (int k = 0; k < 8; ++k) v[k] = sp[(size_t)(g + 64 * k) * h.piece];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) { s1 += v[k].x; far = fmaxf(far, v[k].y); }
-    if (h.mixed) {
-      float u[8];
+      for (int k = 0; k < 8; ++k) { s1 += v[k].x; far = fmaxf(far, v[k].y); }
+      if (h.mixed) {
+        float u[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) u[k] = sp2[(size_t)(g + 16 * k) * h.piece];
+        for (int k = 0; k < 8; ++k) u[k] = sp2[(size_t)(g + 64 * k) * h.piece];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s2 += u[k];
+        for (int k = 0; k < 8; ++k) s2 += u[k];
+      }
     }
+    for (; g < h.groups; g += 64) {
+      const float2 v = sp[(size_t)g * h.piece];
+      s1 += v.x;
+      far = fmaxf(far, v.y);
+      if (h.mixed) s2 += sp2[(size_t)g * h.piece];
+    }
+    s1_s[slice][tid & 15] = s1; s2_s[slice][tid & 15] = s2; top_s[slice][tid & 15] = far;
   }
-  for (; g < h.groups; g += 16) {
-    const float2 v = sp[(size_t)g * h.piece];
-    s1 += v.x;
-    far = fmaxf(far, v.y);
-    if (h.mixed) s2 += sp2[(size_t)g * h.piece];
-  }
-  s1_s[wave][lane] = s1; s2_s[wave][lane] = s2; top_s[wave][lane] = far;
   __syncthreads();
-  if (wave == 0) {
-    for (int w = 1; w < 16; ++w) { s1 += s1_s[w][lane]; s2 += s2_s[w][lane]; far = fmaxf(far, top_s[w][lane]); }
-    s1_s[0][lane] = s1; s2_s[0][lane] = h.mixed ? s2 : s1;
-    // largest exponent, in units of log 2 of the stored exponential; with two softmaxes the second's may be larger
-    const bool single_tau = !h.mixed;
-    const float k = 1.44269504f / (single_tau ? h.tau : 1.f), span = far * 0.693147181f * (single_tau ? 1.f : fmaxf(1.f, 1.f / h.tau));
-    if (!h.again && row < live && span > kFar && far < 1e30f) {
-      h.ref[h.i0 + row] += far / k;
+  if (b0 + wave >= live) return;
+  {
+    const int r = wave;          // a row per wave from here on
+    const float sa = wave_sum(s1_s[lane][r]), st = h.mixed ? wave_sum(s2_s[lane][r]) : sa;          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
+    const float far = wave_max(top_s[lane][r]);
+    // Largest exponent, in units of log 2 of the stored exponential; with two softmaxes the second's may be larger.  Such a row takes its maximum as reference (what the rest of this
+    // kernel makes of it is overwritten when its block is done again).
+    const float span = far * 0.693147181f * (h.mixed ? fmaxf(1.f, 1.f / h.tau) : 1.f);
+    if (!h.again && span > kFar && far < 1e30f && lane == 0) {
+      h.ref[h.i0 + b0 + r] += far * 0.693147181f * (h.mixed ? 1.f : h.tau);
       h.redo[0] = 1;
       h.redo[1 + b0 / 256] = 1;
     }
-  }
-  __syncthreads();
-  for (int r = wave; r < 64 && b0 + r < live; r += 16) {
     const int i = h.i0 + b0 + r, t = h.rows[i];
     const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
     const float ref = h.ref[i], it = 1.0f / h.tau;
-    const float sa = s1_s[0][r], st = s2_s[0][r];          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
     const float* zs = h.zsel + (size_t)i * (h.top + 1);
     const int y = hard ? h.targets[t] : -1;
     const float zy = hard ? zs[h.top] : 0.f;
@@ -531,18 +555,18 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
       h.row_loss[t] = l;
       if (h.row_lse) h.row_lse[t] = ref * it + logf(st);
     }
-    if (!h.e) continue;
+    if (!h.e) return;
     const float g = h.weight ? h.weight[t] : 1.0f / (float)*h.count;
     const float c1 = hard ? g * (1.f - h.share) : 0.f, ct = soft ? g * h.share * h.tau : 0.f;
     const float p1 = c1 / sa, pt = ct / st, C = p1 + pt;          // dz = p1 e1 + pt et - sub
     const float inv = C != 0.f ? 1.0f / C : 0.f;
     if (h.coef && lane == 0) h.coef[b0 + r] = make_float2(p1 * inv, pt * inv);
-    if (!h.places) continue;
+    if (!h.places) return;
     // e at the places, in fp32: the softmaxes' part from the place's logit, less what is taken off there.  The first of equal ids stands for all, in their order; lane 0
     // holds the target in its third slot unless it is among the entries.
 #pragma unroll
     for (int k = 0; k < 2; ++k)
-      if (lane + 64 * k < h.top) { id_s[wave][lane + 64 * k] = id[k]; q_s[wave][lane + 64 * k] = q[k]; }
+      { id_s[wave][lane + 64 * k] = id[k]; q_s[wave][lane + 64 * k] = q[k]; }          // -1 behind the last entry
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): this wave's own list
     auto place = [&](float zv, float sub) {
@@ -552,19 +576,30 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
     int at[3] = {-1, -1, -1};
     float val[3] = {0.f, 0.f, 0.f};
     bool y_listed = false;
-    if (soft)
+    int same[2] = {0, 0};          // entries with this id
+    if (soft) {
+#pragma unroll 4
+      for (int o = 0; o < h.top; o += 4) {
+        const int4 v = *reinterpret_cast<const int4*>(&id_s[wave][o]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) same[k] += (v.x == id[k]) + (v.y == id[k]) + (v.z == id[k]) + (v.w == id[k]);
+      }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int j = lane + 64 * k;
         if (j < h.top && id[k] >= 0) {
-          bool first = true;
-          float sub = id[k] == y ? c1 : 0.f;
           y_listed |= id[k] == y;
-          for (int o = 0; o < h.top; ++o)
-            if (id_s[wave][o] == id[k]) { if (o < j) first = false; sub += ct * q_s[wave][o]; }
-          if (first) { at[k] = id[k]; val[k] = place(zj[k], sub); }
+          bool first = true;
+          float sub = ct * q[k];
+          if (same[k] > 1) {
+            sub = 0.f;
+            for (int o = 0; o < h.top; ++o)
+              if (id_s[wave][o] == id[k]) { if (o < j) first = false; sub += ct * q_s[wave][o]; }
+          }
+          if (first) { at[k] = id[k]; val[k] = place(zj[k], id[k] == y ? sub + c1 : sub); }
         }
       }
+    }
     if (hard && !__ballot(y_listed) && lane == 0) { at[2] = y; val[2] = place(zy, c1); }
     // The row of dz is C e.  Most of its length lies in the largest place (at the target p - 1 against many small p), so C is moved by the at most 2^-8 that make that place's rounded
     // value exact, and the rounding error of the whole gradient is that of its smaller part (128 x 2048, vocab 32000: dX 2.4e-3 -> 1.8e-3 from the exact values, 1.7e-3 of it its own
@@ -578,7 +613,6 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
 #pragma unroll
     for (int k = 0; k < 3; ++k)
       if (at[k] >= 0) e[at[k]] = from_f32<bf16_t>(val[k] * move);
-    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -659,7 +693,7 @@ __global__ __launch_bounds__(256) void head_et_kernel(const bf16_t* __restrict__
 // dz in fp32 and not rounded.  Fixed orders throughout: no atomics.
 struct HeadFew {
   const void *x, *w;
-  int ldx, ldw, n, V, d, ldz, parts, top, dw_lo, dw_hi, lddx, lddw, dw_add, chunk, vec;          // parts: waves of the first kernel; chunk: rows of W per workgroup of the others
+  int ldx, ldw, n, V, d, ldz, parts, top, dw_lo, dw_hi, lddx, lddw, dw_add, chunk;          // parts: waves of the first kernel; chunk: rows of W per workgroup of the others
   const int32_t *targets, *ids;
   const float *logits, *weight;
   float tau, share;
@@ -674,13 +708,28 @@ template <class T> struct FewChunk;          // 16 bytes of a row: 8 bf16 or 4 f
 template <> struct FewChunk<bf16_t> { static constexpr int E = 8; };
 template <> struct FewChunk<float> { static constexpr int E = 4; };
 
-template <class T, bool VEC> __device__ __forceinline__ uint4 few_load(const T* row, int k, int d) {          // elements k .. of a row, zeros from d on
+struct __attribute__((packed, aligned(2))) few_raw { uint32_t w[4]; };          // 16 bytes at any element: the card loads them in one go from any address
+template <class T> __device__ __forceinline__ uint4 few_load(const T* row, int k, int d) {          // elements k .. of a row, zeros from d on
   constexpr int E = FewChunk<T>::E;
-  if (VEC && k + E <= d) return *reinterpret_cast<const uint4*>(row + k);
+  if (k + E <= d) {
+    const few_raw r = *reinterpret_cast<const few_raw*>(row + k);
+    return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+  }
+  if (k >= d) return make_uint4(0, 0, 0, 0);
   union { uint4 u; T e[E]; } r;
 #pragma unroll
   for (int i = 0; i < E; ++i) r.e[i] = k + i < d ? row[k + i] : from_f32<T>(0.f);
   return r.u;
+}
+__device__ __forceinline__ void few_load8(const bf16_t* p, float v[8]) {
+  const few_raw r = *reinterpret_cast<const few_raw*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r.w[i] << 16); v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void few_load8(const float* p, float v[8]) {
+  const few_raw a = *reinterpret_cast<const few_raw*>(p), b = *reinterpret_cast<const few_raw*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a.w[i]); v[4 + i] = __uint_as_float(b.w[i]); }
 }
 __device__ __forceinline__ void few_mfma(few_f32x4& acc, const uint4& a, const uint4& b, bf16_t) {
   acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(few_bf16x8, a), __builtin_bit_cast(few_bf16x8, b), acc, 0, 0, 0);
@@ -701,7 +750,7 @@ __device__ __forceinline__ void few_merge(float& m, float& s, float& s2, float m
   m = top;
 }
 
-template <class T, bool VEC>
+template <class T>
 __global__ __launch_bounds__(256) void head_few_z_kernel(HeadFew h) {
   constexpr int E = FewChunk<T>::E, U = 8, STEP = 4 * E;          // k per MFMA step of the four lane groups
   const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4, gw = blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -714,9 +763,9 @@ __global__ __launch_bounds__(256) void head_few_z_kernel(HeadFew h) {
     uint4 a[2][U], b[2][U];
     auto fetch = [&](int buf, int k0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) a[buf][u] = few_load<T, VEC>(w, k0 + u * STEP + lq * E, h.d);
+      for (int u = 0; u < U; ++u) a[buf][u] = few_load<T>(w, k0 + u * STEP + lq * E, h.d);
 #pragma unroll
-      for (int u = 0; u < U; ++u) b[buf][u] = few_load<T, VEC>(x, k0 + u * STEP + lq * E, h.d);
+      for (int u = 0; u < U; ++u) b[buf][u] = few_load<T>(x, k0 + u * STEP + lq * E, h.d);
     };
     auto multiply = [&](int buf) {
 #pragma unroll
@@ -770,12 +819,22 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
       }
     }
     soft = __ballot(id[0] >= 0 || id[1] >= 0) != 0;
-    for (int g = lane; g < h.parts; g += 64) {
-      const float4 p = *reinterpret_cast<const float4*>(h.part + ((size_t)t * h.parts + g) * 4);
-      few_merge(m, s, s2, p.x, p.y, p.z, it);
-    }
+    // at most 2048 partial sums, 32 a lane: all of them requested at once, the maximum first, then sums that do not wait for each other
+    const float4* part = reinterpret_cast<const float4*>(h.part) + (size_t)t * h.parts;
+    constexpr int K = 2048 / 64;
+    float4 p[K];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) few_merge(m, s, s2, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(s2, o, 64), it);
+    for (int k = 0; k < K; ++k) p[k] = lane + 64 * k < h.parts ? part[lane + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) m = fmaxf(m, p[k].x);
+    m = wave_max(m);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      s += p[k].x == -INFINITY ? p[k].y : p[k].y * expf(p[k].x - m);          // a part without a finite logit has a sum of 0, or NaN
+      if (it != 1.f) s2 += p[k].x == -INFINITY ? p[k].z : p[k].z * expf((p[k].x - m) * it);
+    }
+    s = wave_sum(s);
+    s2 = it == 1.f ? s : wave_sum(s2);
   }
   if (lane == 0) live_s[t] = hard || soft;
   __syncthreads();
@@ -877,7 +936,7 @@ __global__ __launch_bounds__(256) void head_few_dx_kernel(HeadFew h, int cols) {
     auto row = [&](int r) {
       float v[8];
       const T* p = w + (size_t)(v0 + r) * h.ldw + c;
-      if (h.vec && c + 8 <= h.d) load8(p, v);
+      if (c + 8 <= h.d) few_load8(p, v);
       else
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < h.d ? to_f32(p[e]) : 0.f;
@@ -951,18 +1010,27 @@ __global__ __launch_bounds__(256) void head_few_dw_kernel(HeadFew h, int cols) {
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
-// dx[rows[i]] = scale[i] sum of the partials [splits][live64][d], a wave per compact row of the piece
-__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const float* __restrict__ scale, bf16_t* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows,
-                                                          const int32_t* __restrict__ count, int i0, int piece) {
+// dx[rows[i]] = scale[i] (1 without) sum of the partials [splits][pitch][d], a wave per compact row of the piece; pitch 0: the rows that count, in whole groups of 64
+template <class T>
+__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, int pitch, const float* __restrict__ scale, T* __restrict__ dx, int lddx, int d,
+                                                          const int32_t* __restrict__ rows, const int32_t* __restrict__ count, int i0, int piece) {
   const int i = blockIdx.x * 4 + (threadIdx.x >> 6), live = min(max(*count - i0, 0), piece);
   if (i >= live) return;
-  const size_t mn = (size_t)((live + 63) & ~63) * d;
-  const float sc = scale[i0 + i];
+  const size_t mn = (size_t)(pitch ? pitch : (live + 63) & ~63) * d;
+  const float sc = scale ? scale[i0 + i] : 1.f;
   const int t = rows[i0 + i];
   for (int c = threadIdx.x & 63; c < d; c += 64) {
     float s = 0.f;
-    for (int z = 0; z < splits; ++z) s += part[z * mn + (size_t)i * d + c];
-    dx[(size_t)t * lddx + c] = from_f32<bf16_t>(s * sc);
+    int z = 0;
+    for (; z + 4 <= splits; z += 4) {          // four loads in flight
+      float v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = part[(z + k) * mn + (size_t)i * d + c];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s += v[k];
+    }
+    for (; z < splits; ++z) s += part[z * mn + (size_t)i * d + c];
+    dx[(size_t)t * lddx + c] = from_f32<T>(s * sc);
   }
 }
 // out = sum of the partials [splits][rows][d] (+ add), out float or bf16
@@ -977,25 +1045,11 @@ __global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restric
     out[(size_t)r * ldo + c] = from_f32<TO>(s);
   }
 }
-// dx[rows[i]] = dxc[i] for the compact rows of a piece
-template <class T>
-__global__ __launch_bounds__(256) void head_scatter_kernel(const T* __restrict__ dxc, int dp, T* __restrict__ dx, int lddx, int d, const int32_t* __restrict__ rows, const int32_t* __restrict__ count,
-                                                           int i0, int m) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= m || i0 + i >= *count) return;
-  const int t = rows[i0 + i];
-  for (int c = threadIdx.x & 63; c < d; c += 64) dx[(size_t)t * lddx + c] = dxc[(size_t)i * dp + c];
-}
-// out (+)= acc, rows of d; or, with `sum`, sum (+)= acc
 template <class TO>
-__global__ __launch_bounds__(256) void head_add_kernel(const float* __restrict__ acc, TO* out, int ldo, int rows, int d, int add) {
+__global__ __launch_bounds__(256) void head_zero_kernel(TO* out, int ldo, int rows, int d) {
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= rows) return;
-  for (int c = threadIdx.x & 63; c < d; c += 64) {
-    TO* o = out + (size_t)r * ldo + c;
-    const float v = acc ? acc[(size_t)r * d + c] : 0.f;
-    *o = from_f32<TO>(add ? to_f32(*o) + v : v);
-  }
+  for (int c = threadIdx.x & 63; c < d; c += 64) out[(size_t)r * ldo + c] = from_f32<TO>(0.f);
 }
 // loss = sum of weight * row_loss, or their mean over the rows that count (rows that are left out have a row_loss of 0, and their weight is not looked at)
 __global__ __launch_bounds__(1024) void head_loss_kernel(const float* __restrict__ row_loss, const float* __restrict__ weight, const int32_t* __restrict__ count, float* __restrict__ loss, int n) {
@@ -1037,13 +1091,9 @@ static void few_grads(hipStream_t st, const HeadArgs& a, HeadFew h) {
 }
 template <class T>
 static void head_few(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, float* row_loss) {
-  HeadFew h{a.x, a.w, a.ldx, a.ldw, a.n, a.vocab, a.d, p.vp, p.parts, a.top, a.dw_lo, a.dw_hi, a.lddx, a.lddw, a.dw_f32 == 2, 0, 0, a.targets, a.ids, a.logits, a.row_weight, a.tau, a.share,
+  HeadFew h{a.x, a.w, a.ldx, a.ldw, a.n, a.vocab, a.d, p.vp, p.parts, a.top, a.dw_lo, a.dw_hi, a.lddx, a.lddw, a.dw_f32 == 2, 0, a.targets, a.ids, a.logits, a.row_weight, a.tau, a.share,
             (float*)(ws + p.z), (float*)(ws + p.stats), (float*)(ws + p.coef), (float*)(ws + p.scale), (float*)(ws + p.part), (int32_t*)(ws + p.zsel), a.loss, row_loss, a.row_lse, a.dx, a.dw};
-  constexpr int E = FewChunk<T>::E;
-  h.vec = a.ldw % 8 == 0 && ((uintptr_t)a.w & 15) == 0;
-  const bool vec = a.ldw % E == 0 && a.ldx % E == 0 && (((uintptr_t)a.w | (uintptr_t)a.x) & 15) == 0;
-  if (vec) head_few_z_kernel<T, true><<<p.parts / 4, 256, 0, st>>>(h);
-  else head_few_z_kernel<T, false><<<p.parts / 4, 256, 0, st>>>(h);
+  head_few_z_kernel<T><<<p.parts / 4, 256, 0, st>>>(h);
   head_few_fin_kernel<<<1, 1024, 0, st>>>(h);
   if (a.n == 1) few_grads<T, 1>(st, a, h);
   else if (a.n <= 4) few_grads<T, 4>(st, a, h);
@@ -1054,26 +1104,32 @@ static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
   const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
   auto* rows = (int32_t*)(ws + p.rows);
   auto* count = (int32_t*)(ws + p.count);
-  float *dwa = (float*)(ws + p.dwa), *z = (float*)(ws + p.z), *dxc = (float*)(ws + p.dxc);
+  float *z = (float*)(ws + p.z), *part = (float*)(ws + p.part);
   HeadRow h{rows, count, a.targets, a.ids, a.logits, a.row_weight, a.top ? (unsigned char*)(ws + p.flags) : nullptr, row_loss, a.row_lse, a.tau, a.share, a.vocab, p.vp, a.top, 0};
   for (int i0 = 0; i0 < a.n; i0 += p.piece) {
     const int m = std::min(p.piece, p.np - i0);
     const float* xp = (const float*)(ws + p.xc) + (size_t)i0 * p.dp;
-    auto nt = [&](const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K) { k_gemm_nt_f32(st, 0, A, lda, B, ldb, C, ldc, M, N, K, EPI_STORE, nullptr, 1, 1, nullptr); };
     h.i0 = i0;
-    nt(xp, p.dp, w, ldw, z, p.vp, m, a.vocab, a.d);
-    head_row_kernel<float><<<m, 256, 0, st>>>(z, p.grads ? z : nullptr, h);
+    k_gemm_nt_f32(st, 0, xp, p.dp, w, ldw, z, p.vp, m, a.vocab, a.d, EPI_STORE, nullptr, 1, 1, nullptr, count, i0, m);
+    const int g = p.grads;
+    if (p.vp <= 2 * 4 * 256) head_row_kernel<256, 2><<<m, 256, 0, st>>>(z, g, h);
+    else if (p.vp <= 8 * 4 * 256) head_row_kernel<256, 8><<<m, 256, 0, st>>>(z, g, h);
+    else if (p.vp <= 8 * 4 * 1024) head_row_kernel<1024, 8><<<m, 1024, 0, st>>>(z, g, h);
+    else head_row_kernel<1024, 0><<<m, 1024, 0, st>>>(z, g, h);
     if (a.dx) {
-      nt(z, p.vp, wt, ldwt, dxc, p.dp, m, a.d, a.vocab);
-      head_scatter_kernel<float><<<quads(m), 256, 0, st>>>(dxc, p.dp, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
+      k_gemm_nt_f32(st, 0, z, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, EPI_STORE, nullptr, 1, p.dx_splits, part, count, i0, m);
+      head_dx_sum_kernel<float><<<quads(m), 256, 0, st>>>(part, p.dx_splits, m, nullptr, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
     }
     if (a.dw) {
-      const bool first = i0 == 0, last = i0 + p.piece >= a.n;
-      float* prod = first ? dwa : (float*)(ws + p.dwp);
-      // columns that start off a group of four, or rows too long for the token-major kernel's offsets, cannot happen: vp <= 2^20 + 3
-      k_gemm_tn_f32(st, z + a.dw_lo, p.vp, dw_rows, 0, xp, p.dp, prod, a.d, dw_rows, a.d, m, 1, nullptr);
-      if (!first) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(prod, dwa, a.d, dw_rows, a.d, 1);
-      if (last) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(dwa, (float*)a.dw, a.lddw, dw_rows, a.d, a.dw_f32 == 2);
+      // (columns too long for the kernel's offsets cannot happen: vp < 2^20 + 128)
+      const bool add = i0 > 0 || a.dw_f32 == 2;
+      float* dw = (float*)a.dw;
+      if (p.dw_splits == 1 && !add) k_gemm_tn_f32(st, z + a.dw_lo, p.vp, dw_rows, 0, xp, p.dp, dw, a.lddw, dw_rows, a.d, m, 1, nullptr, count, i0, m);
+      else {
+        const int splits = m % (4 * p.dw_splits) == 0 ? p.dw_splits : 1;
+        k_gemm_tn_f32(st, z + a.dw_lo, p.vp, dw_rows, 0, xp, p.dp, part, a.d, dw_rows, a.d, m, splits, part, count, i0, m);
+        head_dw_sum_kernel<float><<<quads(dw_rows), 256, 0, st>>>(part, splits, add ? dw : nullptr, a.lddw, dw, a.lddw, dw_rows, a.d);
+      }
     }
   }
 }
@@ -1090,7 +1146,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
   bf16_t* e = p.grads ? (bf16_t*)(ws + p.z) : nullptr;
   const bf16_t* xc = (const bf16_t*)(ws + p.xc);
   bool ok = true;
-  head_ref_kernel<<<quads(p.np), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
+  head_ref_kernel<<<dim3((p.np + 3) / 4, std::max(1, (a.top + kRefGroup - 1) / kRefGroup)), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
                                                        a.ldx % 8 == 0 && ((uintptr_t)a.x & 15) == 0, (const int32_t*)(ws + p.pos), count, a.targets, a.ids, a.logits, flags, zsel, ref, row_loss, a.row_lse});
   const float log2e = 1.44269504f;
   for (int i0 = 0; i0 < a.n; i0 += p.piece) {
@@ -1102,16 +1158,16 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
               !p.mixed, redo, a.tau, a.share};
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
-    head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+    head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     he.redo = redo;
     f.again = 1;
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
-    head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+    head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     if (!e) continue;
     if (p.mixed) {
       head_mix_kernel<<<m, 256, 0, st>>>(e, p.vp, coef, count, i0, m, 1.0f / a.tau);
       f.again = 0; f.places = 1;
-      head_fin_kernel<<<m / 64, 1024, 0, st>>>(f);
+      head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     }
     he.scale = scale; he.rows = rows;
     if (a.dx) {
@@ -1120,7 +1176,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
         ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, wt, ldwt, a.dx, a.lddx, m, a.d, p.vp, 1, he) == 0;
       else {
         ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, p.dx_splits, he) == 0;
-        head_dx_sum_kernel<<<quads(m), 256, 0, st>>>(part, p.dx_splits, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
+        head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, p.dx_splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
       }
     }
     if (a.dw) {
@@ -1183,8 +1239,8 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   if (p.own_wt) { transpose(a.w, a.ldw, ws + p.wt, p.vp, a.vocab, a.d); wt = ws + p.wt; ldwt = p.vp; }
 
   if (a.n == 0 && a.dw && a.dw_f32 != 2) {
-    if (a.dw_f32) head_add_kernel<float><<<quads(dw_rows), 256, 0, st>>>(nullptr, (float*)a.dw, a.lddw, dw_rows, a.d, 0);
-    else PP_H_DISPATCH(a.dtype, head_add_kernel<T><<<quads(dw_rows), 256, 0, st>>>(nullptr, (T*)a.dw, a.lddw, dw_rows, a.d, 0));
+    if (a.dw_f32) head_zero_kernel<float><<<quads(dw_rows), 256, 0, st>>>((float*)a.dw, a.lddw, dw_rows, a.d);
+    else PP_H_DISPATCH(a.dtype, head_zero_kernel<T><<<quads(dw_rows), 256, 0, st>>>((T*)a.dw, a.lddw, dw_rows, a.d));
   }
   bool ok = true;
   if (a.dtype) ok = head_bf16(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
