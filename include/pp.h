@@ -56,8 +56,13 @@ typedef struct {
   int32_t recompute;          /* 0: every layer's activations are kept for the backward pass.  1: full activation
                                  recomputation (the memory regime of the paper's Table 1): only each layer's input is
                                  kept, the layer is run forward again when the backward pass reaches it.  Same results
-                                 bit for bit; WORKSPACE shrinks by about (n_layers - 1) layers of activations. */
+                                 bit for bit; WORKSPACE shrinks by about (n_layers - 1) layers of activations.
+                                 PP_HEAD_PIECES may be added to either (a bit): the output head's logits are not kept either.  Its loss and gradients
+                                 are formed a piece of rows at a time (pp_op_head_ce in pp_ops.h states how, and the roundings; with bf16 storage the loss is
+                                 formed from fp32 logits, not from rounded ones), WORKSPACE holds at most about 1.5 GiB for them instead of B x S x vocab elements, and
+                                 vocab may be up to 2^20 (without: 65536 with bf16 storage, 16320 with fp32). */
 } pp_config;
+enum { PP_HEAD_PIECES = 4 };
 
 /* I_train of Algorithm 1 as a union of row blocks (Section "Parameter Slicing").
  * all != 0: every parameter is trainable (the full-backprop step) and the other fields are ignored.
@@ -103,7 +108,7 @@ int pp_init_model(const pp_config* cfg, void* params_dev, size_t params_bytes, v
  * offset of every packed row of d_model elements), "shadow.<weight>" (the transposed read-only copy of wqkv, wo,
  * wd or lm_head, shape [in x out]) and, for debugging, "dbg.<buffer>[.<layer>]" taps into the workspace
  * (x, n1, qkv, o, xm, n2, gu, a, lse per layer; xL, logits, dx, dn, dqkv, dgu), sized for max_batch*max_seq tokens;
- * with recompute = 1 only x is per layer, the others show the layer worked on last.
+ * with recompute = 1 only x is per layer, the others show the layer worked on last; with PP_HEAD_PIECES there are no logits.
  * Both block until the copy is done.
  * pp_set_tensor on a weight after pp_set_trainable_mask leaves the fp32 masters stale: set the mask again. */
 int pp_set_tensor(pp_model* m, const char* name, const void* host_src, size_t bytes);
@@ -124,6 +129,11 @@ int pp_set_trainable_mask(pp_model* m, const pp_mask* mask, void* state_dev, siz
  * Asynchronous on the stream.  PP_ESTATE before pp_set_trainable_mask; PP_EINVAL on bad shapes. */
 int pp_local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S,
                   const pp_adamw* opt, float* loss_dev);
+
+/* The same step with the loss of pp_op_head_distill (pp_ops.h) in place of the cross entropy: ids_dev int32 and logits_dev float [B x S x top] are the teacher's top entries of
+ * every position, 1 <= top <= PP_HEAD_TOP_MAX; targets_dev may be NULL if share == 1.  Needs a model with PP_HEAD_PIECES (PP_EINVAL otherwise). */
+int pp_local_step_distill(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S, const int32_t* ids_dev, const float* logits_dev,
+                          int32_t top, float temperature, float share, const pp_adamw* opt, float* loss_dev);
 
 /* Ablation of Appendix "Additional Results" (off by default; the paper reports that it diverges or degrades):
  * which FFN hidden units enter the INPUT gradient of every later pp_local_step.
@@ -170,7 +180,7 @@ int pp_get_counters(pp_model* m, double* flops_fwd, double* flops_bwd, double* a
 int pp_get_launch_counts(pp_model* m, int64_t* matrix_core_calls, int64_t* plain_calls);
 
 /* Options for tests and profiling.  "force_plain": 0 = automatic (MFMA kernels when shapes allow), 1 = force the
- * plain (non-MFMA) kernels throughout.  "dw_tn": 1 (default) = weight-gradient GEMMs read their token-major operands directly
+ * plain (non-MFMA) kernels throughout (the head of PP_HEAD_PIECES has none: it stays as it is).  "dw_tn": 1 (default) = weight-gradient GEMMs read their token-major operands directly
  * (LDS transpose reads), 0 = through transposed copies and the NT kernel.  "fuse_rope": 1 (default) = the rotary embedding of
  * q and k is applied in the q|k|v projection's epilogue (one rounding), 0 = as a separate pass over the stored projection.  "time_gemm": 1 = bracket every GEMM launch of later pp_local_step calls with a pair
  * of HIP events on the model's stream (host-side events only; no device memory), 0 = off; setting it resets the totals.
@@ -185,7 +195,7 @@ int pp_get_launch_counts(pp_model* m, int64_t* matrix_core_calls, int64_t* plain
 int pp_set_option(pp_model* m, const char* key, int64_t value);
 
 /* Blocks until the stream is idle, then returns the summed duration (ms), matmul FLOPs and number of the GEMM
- * launches (forward, input-gradient and weight-gradient GEMMs, split-K reduction included) bracketed since
+ * launches (forward, input-gradient and weight-gradient GEMMs, split-K reduction included; not the head of PP_HEAD_PIECES) bracketed since
  * "time_gemm" was set or since the previous call, and resets the totals. */
 int pp_get_gemm_timing(pp_model* m, double* total_ms, double* total_flops, int64_t* launches);
 

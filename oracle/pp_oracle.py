@@ -184,7 +184,9 @@ def forward(cfg, params, tokens, targets, keep_probs=True):
 
 
 def _dlogits(cache):
-    """dL/dz = (softmax(z) - onehot(target)) / n_valid on valid rows, 0 on ignored rows."""
+    """dL/dz = (softmax(z) - onehot(target)) / n_valid on valid rows, 0 on ignored rows; another loss leaves its own in cache["dlogits"]."""
+    if "dlogits" in cache:
+        return cache["dlogits"]
     z, lse, tg, valid = cache["z"], cache["lse"], cache["targets"], cache["valid"]
     dz = np.exp(z - lse[:, None])
     rows = np.nonzero(valid)[0]
@@ -617,3 +619,12 @@ def head_loss(x, w, targets, row_weight=None, ids=None, logits=None, tau=1.0, sh
         dz[t] *= g[t]
     x0 = np.where(live[:, None], x, 0.0)
     return dict(loss=float(np.sum(np.where(live, g, 0.0) * row_loss)), row_loss=row_loss, row_lse=row_lse, z=z, dz=dz, dx=dz @ w, dw=dz.T @ x0, live=live)
+
+
+def distilled(cfg, params, tokens, targets, mask, ids, logits, tau, share):
+    """Loss and masked gradient of a step whose loss is head_loss's distillation; ids, logits [B, S, top]."""
+    _, cache = forward(cfg, params, tokens, targets)
+    top = ids.shape[-1]
+    h = head_loss(cache["nf"], params["lm_head"], targets.reshape(-1), None, ids.reshape(-1, top), logits.reshape(-1, top), tau, share)
+    cache["dlogits"] = h["dz"]
+    return h["loss"], masked_gradient(cfg, params, cache, mask)

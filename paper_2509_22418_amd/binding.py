@@ -14,8 +14,9 @@ import numpy as np
 PP_F32, PP_BF16 = 0, 1
 PP_STATIC_SCRATCH_FLOATS = 4 << 20          # include/pp_ops.h
 PP_HEAD_TOP_MAX = 128                       # include/pp_ops.h
+PP_HEAD_PIECES = 4                          # include/pp.h
 PP_BYTES_PARAMS, PP_BYTES_STATE, PP_BYTES_WORKSPACE, PP_BYTES_SHADOW, PP_BYTES_ACTIVATIONS = range(5)
-EXPORTS = ["pp_query_bytes", "pp_init_model", "pp_set_tensor", "pp_get_tensor", "pp_set_trainable_mask", "pp_local_step",
+EXPORTS = ["pp_query_bytes", "pp_init_model", "pp_set_tensor", "pp_get_tensor", "pp_set_trainable_mask", "pp_local_step", "pp_local_step_distill",
            "pp_set_jacobian_slices", "pp_outer_delta", "pp_outer_delta_group", "pp_synth_delta_sum", "pp_get_counters", "pp_get_launch_counts", "pp_get_gemm_timing", "pp_set_option", "pp_last_error", "pp_free",
            "pp_op_gemm_nt", "pp_op_gemm_tn", "pp_op_gemm_nt_splitk_static", "pp_op_attention_fwd", "pp_op_attention_bwd",
            "pp_op_head_bytes", "pp_op_head_ce", "pp_op_head_distill"]
@@ -79,6 +80,8 @@ def load_library():
     lib.pp_set_trainable_mask.argtypes = [vp, C.POINTER(PPMask), vp, sz]
     lib.pp_local_step.restype = C.c_int
     lib.pp_local_step.argtypes = [vp, vp, vp, i32, i32, C.POINTER(PPAdamW), vp]
+    lib.pp_local_step_distill.restype = C.c_int
+    lib.pp_local_step_distill.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, C.c_float, C.c_float, C.POINTER(PPAdamW), vp]
     lib.pp_outer_delta.restype = C.c_int
     lib.pp_outer_delta.argtypes = [vp, vp, vp, vp, C.POINTER(PPOuter), vp]
     lib.pp_set_jacobian_slices.restype = C.c_int
@@ -164,6 +167,11 @@ def pp_set_trainable_mask(h, mask: PPMask, state_ptr: int, state_bytes: int):
 
 def pp_local_step(h, tokens_ptr: int, targets_ptr: int, B: int, S: int, opt, loss_ptr: int):
     _check(load_library().pp_local_step(h, tokens_ptr, targets_ptr, B, S, None if opt is None else C.byref(opt), loss_ptr), "pp_local_step")
+
+
+def pp_local_step_distill(h, tokens_ptr: int, targets_ptr, B: int, S: int, ids_ptr: int, logits_ptr: int, top: int, temperature: float, share: float, opt, loss_ptr: int):
+    _check(load_library().pp_local_step_distill(h, tokens_ptr, targets_ptr, B, S, ids_ptr, logits_ptr, top, temperature, share, None if opt is None else C.byref(opt), loss_ptr),
+           "pp_local_step_distill")
 
 
 def pp_set_jacobian_slices(h, mode: int, extra_lo: int = 0, extra_hi: int = 0):
@@ -279,7 +287,8 @@ def make_head(x, w, *, row_weight=None, loss=None, row_loss=None, row_lse=None, 
 # --------------------------------------------------------------------------------------------- convenience holder
 def make_config(cfg: dict) -> PPConfig:
     return PPConfig(cfg["n_layers"], cfg["d_model"], cfg["n_heads"], cfg["d_ff"], cfg["vocab"], cfg.get("max_batch", cfg["batch"]),
-                    cfg.get("max_seq", cfg["seq"]), PP_BF16 if cfg["dtype"] == "bf16" else PP_F32, cfg["rms_eps"], cfg["rope_base"], int(cfg.get("recompute", 0)))
+                    cfg.get("max_seq", cfg["seq"]), PP_BF16 if cfg["dtype"] == "bf16" else PP_F32, cfg["rms_eps"], cfg["rope_base"],
+                    int(cfg.get("recompute", 0)) | (PP_HEAD_PIECES if cfg.get("head_pieces") else 0))
 
 
 def make_mask(mask: dict) -> PPMask:
@@ -376,6 +385,17 @@ class LocalStepModel:
         B, S = tokens_dev.shape
         opt = None if hp is None else PPAdamW(hp["lr"], hp["beta1"], hp["beta2"], hp["eps"], hp["weight_decay"])
         pp_local_step(self.h, tokens_dev.data_ptr(), targets_dev.data_ptr(), B, S, opt, self.loss.data_ptr())
+        return self.loss
+
+    def step_distill(self, tokens_dev, targets_dev, ids_dev, logits_dev, temperature: float, share: float, hp: dict | None):
+        """step() with the distillation loss (a model with head_pieces): ids_dev int32 and logits_dev float32 [B, S, top]; targets_dev may be None if share == 1."""
+        B, S, top = ids_dev.shape
+        t = self.torch
+        if tuple(tokens_dev.shape) != (B, S) or tuple(logits_dev.shape) != (B, S, top) or ids_dev.dtype != t.int32 or logits_dev.dtype != t.float32 or not ids_dev.is_contiguous() or not logits_dev.is_contiguous():
+            raise PPError("step_distill: ids must be contiguous int32 and logits contiguous float32, both [B, S, top]")
+        opt = None if hp is None else PPAdamW(hp["lr"], hp["beta1"], hp["beta2"], hp["eps"], hp["weight_decay"])
+        pp_local_step_distill(self.h, tokens_dev.data_ptr(), None if targets_dev is None else targets_dev.data_ptr(), B, S, ids_dev.data_ptr(), logits_dev.data_ptr(), top, temperature, share,
+                              opt, self.loss.data_ptr())
         return self.loss
 
     def counters(self):

@@ -2,6 +2,7 @@
 // local step (forward over all parameters, restricted backward, AdamW on the trainable subset) and of the
 // outer pseudo-gradient step.  All device memory belongs to the caller; see include/pp.h.
 #include "../../include/pp.h"
+#include "../../include/pp_ops.h"
 #include "pp_kernels.h"
 
 #include <algorithm>
@@ -80,17 +81,33 @@ struct WsPlan {          // byte offsets into the workspace
   size_t rope_cos, rope_sin, shadow, rows, segs, keys;
   size_t act0, act_stride;          // per layer (recompute: the layer input only)
   size_t act_shared;                // recompute: the one block that holds the other activations of the layer in work
-  bool recompute;
+  bool recompute, pieces;
   size_t a_x, a_n1, a_qkv, a_o, a_xm, a_n2, a_gu, a_a, a_rstd1, a_rstd2, a_lse;      // within a layer's block
   size_t xL, nf, rstdf, logits, rowloss, nvalid, dgpart;
   size_t dx, dn, dA, dgu, dob, dqkv, Dattn;
   size_t fixed_end;      // everything above is mask independent
-  size_t tA, tB, partial, partial_bytes, total;
+  size_t tA, tB, partial, partial_bytes, head, head_bytes, total;          // head: of the losses in pieces
   size_t act_bytes, shadow_bytes;
 };
 
 static size_t esize(const pp_config& c) { return c.dtype == PP_F32 ? 4 : 2; }
 static const size_t kPartialCap = 64ull << 20;
+
+// The head's losses inside the step: sizes and options of a call of n rows (its pointers are filled in by the step; those that decide about the workspace are not NULL here)
+static HeadArgs step_head(const pp_config& c, bool dw, bool dx, int n) {
+  HeadArgs a{};
+  static const char some[64] __attribute__((aligned(256))) = {0};
+  a.x = a.w = a.wt = some;
+  a.dx = dx ? (void*)some : nullptr;
+  a.dw = dw ? (void*)some : nullptr;
+  a.ldx = a.ldw = a.lddx = a.lddw = a.d = c.d_model;
+  a.dtype = c.dtype; a.n = n; a.vocab = c.vocab; a.ldwt = c.vocab;
+  a.dw_hi = dw ? c.vocab : 0; a.dw_f32 = 1;
+  a.tau = 1.f;
+  a.part_cap = kPartialCap;
+  a.no_few = 1;
+  return a;
+}
 
 static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
   WsPlan p{};
@@ -112,7 +129,8 @@ static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
   p.a_x = ltake(T * d * es); p.a_n1 = ltake(T * d * es); p.a_qkv = ltake(T * 3 * d * es); p.a_o = ltake(T * d * es);
   p.a_xm = ltake(T * d * es); p.a_n2 = ltake(T * d * es); p.a_gu = ltake(T * 2 * F * es); p.a_a = ltake(T * F * es);
   p.a_rstd1 = ltake(T * 4); p.a_rstd2 = ltake(T * 4); p.a_lse = ltake((size_t)c.max_batch * h * c.max_seq * 4);
-  p.recompute = c.recompute != 0;
+  p.recompute = (c.recompute & 1) != 0;
+  p.pieces = (c.recompute & PP_HEAD_PIECES) != 0;
   if (p.recompute) {          // per layer: x only (a_x = 0 is the first field of the block); everything else lives once
     p.act_stride = align_up(T * d * es);
     p.act0 = take(p.act_stride * c.n_layers);
@@ -122,7 +140,7 @@ static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
     p.act0 = take(p.act_stride * c.n_layers);
     p.act_shared = 0;
   }
-  p.xL = take(T * d * es); p.nf = take(T * d * es); p.rstdf = take(T * 4); p.logits = take(T * V * es);
+  p.xL = take(T * d * es); p.nf = take(T * d * es); p.rstdf = take(T * 4); p.logits = take(p.pieces ? 0 : T * V * es);
   p.act_bytes = off - p.act0;
   p.rowloss = take(T * 4); p.nvalid = take(256); p.dgpart = take(64 * d * 4);
   p.dx = take(T * d * es); p.dn = take(T * d * es); p.dA = take(T * F * es); p.dgu = take(T * 2 * F * es);
@@ -135,12 +153,18 @@ static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
   if (m.ffn) rowsA = std::max(rowsA, (size_t)2 * (m.fh - m.fl));
   if (m.heads) rowsA = std::max(rowsA, (size_t)3 * (m.hh - m.hl) * dh);
   if (m.wo) rowsA = std::max(rowsA, d);
-  if (m.lm) rowsA = std::max(rowsA, V);
+  if (m.lm && !p.pieces) rowsA = std::max(rowsA, V);
   const bool any_dw = rowsA > 0;
   p.tA = take(rowsA * T * es);
   p.tB = take(any_dw ? d * T * es : 0);
   p.partial_bytes = any_dw ? kPartialCap : 0;
   p.partial = take(p.partial_bytes);
+  if (p.pieces) {
+    HeadArgs a = step_head(c, m.lm, true, (int)T);
+    a.top = PP_HEAD_TOP_MAX;
+    p.head_bytes = head_bytes(a);
+    p.head = take(p.head_bytes);
+  }
   p.total = off;
   return p;
 }
@@ -202,12 +226,15 @@ static int check_cfg(const pp_config* c) {
   if (c->n_layers < 1 || c->d_model < 8 || c->n_heads < 1 || c->d_ff < 8 || c->vocab < 8 || c->max_batch < 1 || c->max_seq < 1)
     return fail(PP_EINVAL, "config: non-positive dimension");
   if (c->dtype != PP_F32 && c->dtype != PP_BF16) return fail(PP_EINVAL, "config: dtype must be PP_F32 or PP_BF16");
-  if (c->recompute != 0 && c->recompute != 1) return fail(PP_EINVAL, "config: recompute must be 0 or 1");
+  if (c->recompute & ~(1 | PP_HEAD_PIECES)) return fail(PP_EINVAL, "config: recompute must be 0 or 1, or one of them plus PP_HEAD_PIECES");
+  const bool pieces = (c->recompute & PP_HEAD_PIECES) != 0;
   if (c->d_model % c->n_heads) return fail(PP_EINVAL, "config: d_model must be a multiple of n_heads");
   const int dh = c->d_model / c->n_heads;
   if (dh % 2 || dh > 256) return fail(PP_EINVAL, "config: head dim must be even and <= 256");
   if (c->d_model % 8 || c->d_ff % 8 || c->vocab % 8) return fail(PP_EINVAL, "config: d_model, d_ff and vocab must be multiples of 8");
-  if (!ce_row_fits(c->dtype, c->vocab))
+  if (pieces && (c->vocab > 1 << 20 || c->d_model > 1 << 14 || (double)c->max_batch * c->max_seq > 1 << 24))
+    return fail(PP_EINVAL, "config: with PP_HEAD_PIECES vocab must be <= 2^20, d_model <= 2^14 and max_batch * max_seq <= 2^24");
+  if (!pieces && !ce_row_fits(c->dtype, c->vocab))
     return fail(PP_EINVAL, c->dtype == PP_BF16 ? "config: vocab > 65536 is not supported by the cross-entropy kernels (bf16)"
                                                : "config: vocab row does not fit the cross-entropy LDS stage (fp32: vocab <= 16320)");
   if (c->max_seq > 8192) return fail(PP_EINVAL, "config: max_seq > 8192 not supported");
@@ -417,6 +444,7 @@ extern "C" int pp_get_tensor(pp_model* m, const char* name, void* host_dst, size
     else if (b == "a") { src = lb + m->ws.a_a; want = T * F * es; }
     else if (b == "lse") { src = lb + m->ws.a_lse; want = (size_t)c.max_batch * c.n_heads * c.max_seq * 4; }
     else if (b == "xL") { src = m->wsp + m->ws.xL; want = T * d * es; }
+    else if (b == "logits" && m->ws.pieces) return fail(PP_EINVAL, "pp_get_tensor: the logits are not kept (PP_HEAD_PIECES)");
     else if (b == "logits") { src = m->wsp + m->ws.logits; want = T * (size_t)c.vocab * es; }
     else if (b == "dx") { src = m->wsp + m->ws.dx; want = T * d * es; }
     else if (b == "dn") { src = m->wsp + m->ws.dn; want = T * d * es; }
@@ -651,9 +679,11 @@ static void attn_bwd(pp_model* m, const void* qkv, const void* o, const float* l
 }
 
 // ------------------------------------------------------------------------------------------------ the local step
-extern "C" int pp_local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S,
-                             const pp_adamw* opt, float* loss_dev) {
-  if (!m || !tokens_dev || !targets_dev || !loss_dev) return fail(PP_EINVAL, "pp_local_step: NULL pointer");
+namespace {
+struct Distill { const int32_t* ids; const float* logits; int top; float tau, share; };
+}
+// kd: the loss of pp_local_step_distill (arguments checked there), nullptr: cross entropy
+static int local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S, const Distill* kd, const pp_adamw* opt, float* loss_dev) {
   if (!m->has_mask) return fail(PP_ESTATE, "pp_local_step: call pp_set_trainable_mask first");
   const pp_config& c = m->cfg;
   if (B < 1 || S < 1 || B > c.max_batch || S > c.max_seq) return fail(PP_EINVAL, "pp_local_step: B or S outside [1, max]");
@@ -711,33 +741,53 @@ extern "C" int pp_local_step(pp_model* m, const int32_t* tokens_dev, const int32
   void* logits = W + w.logits;
   float* rstdf = (float*)(W + w.rstdf);
   k_rmsnorm_fwd(st, dt, xL, canon(ly.final_norm), nf, rstdf, T, d, c.rms_eps);
-  gemm_nt(m, nf, d, canon(ly.lm_head), d, logits, V, T, V, d);
-  int32_t* nvalid = (int32_t*)(W + w.nvalid);
-  float* rowloss = (float*)(W + w.rowloss);
-  k_count_valid(st, targets_dev, T, V, nvalid);
-  if (k_cross_entropy(st, dt, logits, targets_dev, nvalid, rowloss, T, V)) return fail(PP_EINVAL, "pp_local_step: vocab too large for cross entropy kernel");
-  k_loss_reduce(st, rowloss, nvalid, loss_dev, T);
+  const bool any_layer = mk.norms || mk.heads || mk.wo || mk.ffn;
+  void* dn = W + w.dn;
+  float* g = m->sg;
+  if (w.pieces) {          // losses and gradients of the head, its logits a piece at a time
+    HeadArgs h = step_head(c, mk.lm, any_layer || mk.emb, T);
+    h.x = nf; h.w = canon(ly.lm_head); h.wt = shad(ly.sh_lm_head);
+    h.loss = loss_dev; h.row_loss = (float*)(W + w.rowloss);
+    if (h.dx) h.dx = dn;
+    if (h.dw) h.dw = g + find_seg(m, TK_LM_HEAD, -1)->packed_off;
+    h.targets = targets_dev;
+    if (kd) { h.ids = kd->ids; h.logits = kd->logits; h.top = kd->top; h.tau = kd->share > 0.f ? kd->tau : 1.f; h.share = kd->share; if (kd->share == 1.f) h.targets = nullptr; }
+    HeadArgs few = h;
+    few.no_few = 0; few.part_cap = 0;
+    if (head_is_few(few) && head_bytes(few) <= w.head_bytes) h = few;
+    if (k_head(st, h, W + w.head) != 0) return fail(PP_EHIP, "pp_local_step: a kernel of the head could not be set up on this device");
+    const double product = 2.0 * T * (double)V * d;
+    const int grads = (h.dx ? 1 : 0) + (h.dw ? 1 : 0);
+    m->flops_fwd += product; m->flops_bwd += product * grads;
+    if (dt == PP_F32) m->n_plain += 1 + grads;
+    else if (head_is_few(h)) { m->n_mfma += 1; m->n_plain += grads; }
+    else m->n_mfma += 1 + grads;
+  } else {
+    gemm_nt(m, nf, d, canon(ly.lm_head), d, logits, V, T, V, d);
+    int32_t* nvalid = (int32_t*)(W + w.nvalid);
+    float* rowloss = (float*)(W + w.rowloss);
+    k_count_valid(st, targets_dev, T, V, nvalid);
+    if (k_cross_entropy(st, dt, logits, targets_dev, nvalid, rowloss, T, V)) return fail(PP_EINVAL, "pp_local_step: vocab too large for cross entropy kernel");
+    k_loss_reduce(st, rowloss, nvalid, loss_dev, T);
+  }
 
   // ---------------- restricted backward (Appendix "Partial Backward"): dW only for trainable row blocks, dX through
   // every slice and head, nothing below the lowest trainable parameter.
   m->flop_acc = &m->flops_bwd;
-  const bool any_layer = mk.norms || mk.heads || mk.wo || mk.ffn;
   auto below_layer = [&](int l) { return mk.emb || (l > 0 && any_layer); };
   void* dx = W + w.dx;
-  void* dn = W + w.dn;
   void* dA = W + w.dA;
   void* dgu = W + w.dgu;
   void* dob = W + w.dob;
   void* dqkv = W + w.dqkv;
   float* Dattn = (float*)(W + w.Dattn);
   float* dgpart = (float*)(W + w.dgpart);
-  float* g = m->sg;
   void* dz = logits;
   bool reached_bottom = false;
   if (any_layer || mk.emb || mk.lm) {
-    if (mk.lm) gemm_dw_tn(m, dz, V, V, 0, nf, d, g + find_seg(m, TK_LM_HEAD, -1)->packed_off, V, d, T);
+    if (mk.lm && !w.pieces) gemm_dw_tn(m, dz, V, V, 0, nf, d, g + find_seg(m, TK_LM_HEAD, -1)->packed_off, V, d, T);
     if (any_layer || mk.emb) {
-      gemm_nt(m, dz, V, shad(ly.sh_lm_head), V, dn, d, T, d, V);
+      if (!w.pieces) gemm_nt(m, dz, V, shad(ly.sh_lm_head), V, dn, d, T, d, V);
       if (mk.norms) k_rmsnorm_dgamma(st, dt, dn, xL, rstdf, dgpart, g + find_seg(m, TK_FINAL_NORM, -1)->packed_off, T, d);
       k_rmsnorm_bwd(st, dt, dn, xL, rstdf, canon(ly.final_norm), nullptr, dx, T, d);
       for (int l = L - 1; l >= 0; --l) {
@@ -825,6 +875,27 @@ extern "C" int pp_local_step(pp_model* m, const int32_t* tokens_dev, const int32
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(PP_EHIP, std::string("pp_local_step: ") + hipGetErrorString(e));
   return PP_OK;
+}
+
+extern "C" int pp_local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S,
+                             const pp_adamw* opt, float* loss_dev) {
+  if (!m || !tokens_dev || !targets_dev || !loss_dev) return fail(PP_EINVAL, "pp_local_step: NULL pointer");
+  return local_step(m, tokens_dev, targets_dev, B, S, nullptr, opt, loss_dev);
+}
+static int check_distill(const char* who, bool pointers, int top, float temperature, float share) {
+  if (top < 1 || top > PP_HEAD_TOP_MAX) return fail(PP_EINVAL, std::string(who) + ": top outside [1, " + std::to_string(PP_HEAD_TOP_MAX) + "]");
+  if (!(temperature >= 0.015625f && temperature <= 64.f)) return fail(PP_EINVAL, std::string(who) + ": temperature outside [2^-6, 2^6]");
+  if (!(share >= 0.f && share <= 1.f)) return fail(PP_EINVAL, std::string(who) + ": share outside [0, 1]");
+  if (!pointers) return fail(PP_EINVAL, std::string(who) + ": NULL pointer (targets may be NULL only if share == 1)");
+  return PP_OK;
+}
+extern "C" int pp_local_step_distill(pp_model* m, const int32_t* tokens_dev, const int32_t* targets_dev, int32_t B, int32_t S, const int32_t* ids_dev, const float* logits_dev,
+                                     int32_t top, float temperature, float share, const pp_adamw* opt, float* loss_dev) {
+  if (!m || !tokens_dev || !loss_dev) return fail(PP_EINVAL, "pp_local_step_distill: NULL pointer");
+  if (int rc = check_distill("pp_local_step_distill", ids_dev && logits_dev && (targets_dev || share == 1.f), top, temperature, share)) return rc;
+  if (!(m->cfg.recompute & PP_HEAD_PIECES)) return fail(PP_EINVAL, "pp_local_step_distill: the model needs PP_HEAD_PIECES in pp_config.recompute");
+  const Distill kd{ids_dev, logits_dev, top, temperature, share};
+  return local_step(m, tokens_dev, targets_dev, B, S, &kd, opt, loss_dev);
 }
 
 // ------------------------------------------------------------------------------------------------ outer step
@@ -921,7 +992,6 @@ extern "C" int pp_get_launch_counts(pp_model* m, int64_t* matrix_core_calls, int
 }
 
 // ------------------------------------------------------------------------------------------------ op-level entry points
-#include "../../include/pp_ops.h"
 
 extern "C" int pp_op_gemm_nt(void* hip_stream, int dtype, const void* A, int lda, const void* B, int ldb, void* C, int ldc,
                              int M, int N, int K, const void* R, int out_f32, int splits, float* scratch, int path) {
@@ -1064,7 +1134,7 @@ static int check_head(const pp_head* h, int top, HeadArgs* a) {
   if (((uintptr_t)h->x | (uintptr_t)h->w | (uintptr_t)h->dx) & al) return fail(PP_EINVAL, "head: x, w or dx is not aligned to its elements");
   if (dw && (uintptr_t)h->dw & (h->dw_f32 ? 3 : al)) return fail(PP_EINVAL, "head: dw is not aligned to its elements");
   *a = HeadArgs{h->x, h->w, h->row_weight, h->loss, h->row_loss, h->row_lse, h->dx, dw ? h->dw : nullptr, h->ldx, h->ldw, h->lddx, h->lddw, h->dtype, h->n, h->vocab, h->d,
-                h->dw_lo, h->dw_hi, h->dw_f32, h->piece, nullptr, nullptr, nullptr, top, 1.f, 0.f, nullptr, 0};
+                h->dw_lo, h->dw_hi, h->dw_f32, h->piece, nullptr, nullptr, nullptr, top, 1.f, 0.f, nullptr, 0, 0, 0};
   return PP_OK;
 }
 static int run_head(const char* who, void* hip_stream, const HeadArgs& a, void* ws, size_t ws_bytes) {
@@ -1096,11 +1166,8 @@ extern "C" int pp_op_head_ce(void* hip_stream, const pp_head* head, const int32_
 extern "C" int pp_op_head_distill(void* hip_stream, const pp_head* head, const int32_t* ids, const float* logits, int32_t top, float temperature, float share,
                                   const int32_t* targets, void* ws, size_t ws_bytes) {
   HeadArgs a;
-  if (top < 1) return fail(PP_EINVAL, "head: top outside [1, " + std::to_string(PP_HEAD_TOP_MAX) + "]");
-  if (int rc = check_head(head, top, &a)) return rc;
-  if (!(temperature >= 0.015625f && temperature <= 64.f)) return fail(PP_EINVAL, "pp_op_head_distill: temperature outside [2^-6, 2^6]");
-  if (!(share >= 0.f && share <= 1.f)) return fail(PP_EINVAL, "pp_op_head_distill: share outside [0, 1]");
-  if (a.n > 0 && (!ids || !logits || (share < 1.f && !targets))) return fail(PP_EINVAL, "pp_op_head_distill: NULL pointer (targets may be NULL only if share == 1)");
+  if (int rc = check_head(head, std::max(top, 0), &a)) return rc;
+  if (int rc = check_distill("pp_op_head_distill", a.n == 0 || (ids && logits && (share == 1.f || targets)), top, temperature, share)) return rc;
   a.targets = share < 1.f ? targets : nullptr; a.ids = ids; a.logits = logits; a.tau = share > 0.f ? temperature : 1.f; a.share = share;
   return run_head("pp_op_head_distill", hip_stream, a, ws, ws_bytes);
 }

@@ -42,10 +42,11 @@ int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
 // K ranges of a product of `tiles` 256 x 256 tiles and `steps` steps of 64: the number that fills rounds of 256 workgroups best.  A tile's step takes about 0.5 us and a workgroup 4 us
 // besides; every range costs a write and a read of the M x N floats (at 4 TB/s).
-int best_splits(long tiles, long steps, double mn) {
+int best_splits(long tiles, long steps, double mn, size_t cap) {
   int best = 1;
   double cost = 0;
   for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
+    if (s > 1 && cap && s * mn * 4 > (double)cap) break;
     const double c = (double)((tiles * s + 255) / 256) * (0.5 * ((steps + s - 1) / s) + 4) + (s > 1 ? 4 + s * mn * 8 / 4e6 : 0);
     if (s == 1 || c < cost) { best = s; cost = c; }
   }
@@ -71,7 +72,7 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.dp = pad_to(a.d, bf ? 64 : 4);
   p.vp = pad_to(a.vocab, unit);
   p.np = std::max(64, pad_to(a.n, 64));
-  if (a.n > 0 && a.n <= kFew) {
+  if (a.n > 0 && a.n <= kFew && !a.no_few) {
     // up to 2048 waves, 8 a compute unit, each with as many of the blocks of 16 rows of W as any other
     const int tiles = (a.vocab + 15) / 16, each = (tiles + 2047) / 2048;
     p.parts = ((tiles + each - 1) / each + 3) / 4 * 4;
@@ -99,8 +100,8 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !(a.wt && a.vocab % unit == 0 && a.ldwt % 8 == 0 && ((uintptr_t)a.wt & 15) == 0);
   const long tiles_d = (a.d + 255) / 256;
-  p.dx_splits = bf && a.dx ? best_splits((p.piece + 255) / 256 * tiles_d, p.vp / 64, (double)p.piece * a.d) : 1;
-  p.dw_splits = bf && a.dw ? best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, (double)dw_rows * a.d) : 1;
+  p.dx_splits = bf && a.dx ? best_splits((p.piece + 255) / 256 * tiles_d, p.vp / 64, (double)p.piece * a.d, a.part_cap) : 1;
+  p.dw_splits = bf && a.dw ? best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, (double)dw_rows * a.d, a.part_cap) : 1;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
   p.flags = take(a.top ? p.np : 0);
@@ -123,22 +124,27 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.redo = take((size_t)p.n_redo * 4);
     p.dzt = take(a.dw ? (size_t)(dw_rows + 8) * p.piece * es : 0);
     p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
-    p.part = take(std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
+    p.part = take(a.part_cap ? a.part_cap : std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
     p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
   } else {
     // ranges of the contractions: doubled until the products have two workgroups of 32 x 32 tiles for a compute unit
-    auto double_up = [](long tiles, int k, int unit_k) { int s = 1; while (s < 32 && tiles * s < 512 && k % (2 * s * unit_k) == 0 && k / (2 * s) >= 256) s *= 2; return s; };
+    auto double_up = [&](long tiles, int k, int unit_k, size_t out) {
+      int s = 1;
+      while (s < 32 && tiles * s < 512 && k % (2 * s * unit_k) == 0 && k / (2 * s) >= 256 && (!a.part_cap || 2 * s * out <= a.part_cap)) s *= 2;
+      return s;
+    };
     const long t32 = (a.d + 31) / 32;
-    p.dx_splits = a.dx ? double_up((p.piece + 31) / 32 * t32, p.vp, 4) : 1;
-    p.dw_splits = a.dw ? double_up((dw_rows + 31) / 32 * t32, p.piece, 4) : 1;
+    p.dx_splits = a.dx ? double_up((p.piece + 31) / 32 * t32, p.vp, 4, (size_t)p.piece * a.d * 4) : 1;
+    p.dw_splits = a.dw ? double_up((dw_rows + 31) / 32 * t32, p.piece, 4, (size_t)dw_rows * a.d * 4) : 1;
     p.z = take((size_t)p.piece * p.vp * 4);
-    p.part = take(std::max(a.dx ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 || p.piece < a.n || a.dw_f32 == 2 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
+    p.part = take(std::max({a.part_cap, a.dx ? (size_t)p.dx_splits * p.piece * a.d * 4 : (size_t)0, p.dw_splits > 1 || p.piece < a.n || a.dw_f32 == 2 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : (size_t)0}));
   }
   p.total = off;
   return p;
 }
 }  // namespace
 size_t head_bytes(const HeadArgs& a) { return plan_head(a).total; }
+bool head_is_few(const HeadArgs& a) { return plan_head(a).parts > 0; }
 
 // ------------------------------------------------------------------------------------------------ rows that count
 enum { ROW_HARD = 1, ROW_SOFT = 2 };

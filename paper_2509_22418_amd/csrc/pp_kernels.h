@@ -136,6 +136,8 @@ struct HeadArgs {
   float tau, share;                // share of the distillation term (0 where top == 0)
   const void* wt;                  // W^T [d x vocab] (rows of ldwt) that the caller keeps, or nullptr
   int ldwt;
+  size_t part_cap;                 // != 0: partial sums of ranges of a contraction take this many bytes, and fewer ranges are made where they would take more; the size is then monotone in n ...
+  int no_few;                      // ... but for the kernels of few rows, which this keeps away
 };
 // What the head's products on the bf16 matrix cores read besides their operands.  The number of rows that count is on the device only: live = clamp(*count - i0, 0, piece), and
 // whole groups of 64 rows are worked on (rows behind the last one that counts are zeros in every operand).
@@ -163,6 +165,7 @@ struct HeadEpi {
 // the rows that count.  Returns 0 if launched, 1 if not.
 int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he);
 size_t head_bytes(const HeadArgs& a);
+bool head_is_few(const HeadArgs& a);          // whether the kernels of few rows run
 int k_head(hipStream_t st, const HeadArgs& a, char* ws);          // ws: head_bytes(a), 256-byte aligned; 0, or 1 if a kernel cannot be launched
 
 }  // namespace pp

@@ -155,3 +155,25 @@ def test_make_head_checks_its_tensors():
         args = dict(dict(x=x, w=w), **bad)
         with pytest.raises(pp.PPError, match="make_head"):
             pp.make_head(args.pop("x"), args.pop("w"), **args)
+
+
+def test_model_without_kept_logits_plans_less_and_takes_larger_vocabularies():
+    import pp_inputs as gen
+    from paper_2509_22418_amd import binding as b
+    cfg = gen.make_config("1p3b")
+    ask = lambda c, which=b.PP_BYTES_WORKSPACE: b.pp_query_bytes(b.make_config(c), b.make_mask(gen.ffn_slice_mask(cfg, 0, 32)), which)  # noqa: E731
+    kept, pieces = ask(cfg), ask(dict(cfg, head_pieces=1))
+    logits = 8 * 2048 * 32000 * 2
+    assert kept - pieces >= logits // 4
+    assert ask(dict(cfg, head_pieces=1, recompute=1)) < ask(dict(cfg, recompute=1))
+    assert ask(dict(cfg, head_pieces=1), b.PP_BYTES_SHADOW) == ask(cfg, b.PP_BYTES_SHADOW)
+    for c in (dict(cfg, vocab=128000), dict(gen.make_config("tiny"), vocab=20000)):
+        with pytest.raises(pp.PPError, match="vocab"):
+            ask(c)
+        assert ask(dict(c, head_pieces=1)) > 0
+    with pytest.raises(pp.PPError, match="vocab"):
+        ask(dict(cfg, vocab=(1 << 20) + 8, head_pieces=1))
+    lib = b.load_library()
+    for bad in (2, 3, 6, 8, -1):
+        c = b.make_config(dict(cfg, recompute=bad))
+        assert lib.pp_query_bytes(ctypes.byref(c), None, 0) == 0 and "recompute" in b.pp_last_error()
