@@ -206,17 +206,20 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   const int z = blockIdx.y;
   int krange = Ksplit;          // of this workgroup
   size_t kbase = (size_t)z * Ksplit;
-  int live = 0;
+  // Head: BK_FIRST, B lies contraction index first and its fragments are gathered by LDS transpose reads; SWAP, the product is stored transposed, and the MFMAs' operands are
+  // exchanged so that a lane holds four consecutive elements of a row of what is stored.
+  constexpr bool BK_FIRST = EPI >= EPI_HEAD_DX, SWAP = EPI == EPI_HEAD_DW || EPI == EPI_HEAD_DW_PART;
+  int live = 0, klast = 0;          // klast: rows of B in the last step
   if constexpr (EPI >= EPI_HEAD_EXP) {
     if (EPI == EPI_HEAD_EXP && he.redo && he.redo[0] == 0) return;
-    live = min(max(*he.count - he.i0, 0), he.piece);
+    live = __builtin_amdgcn_readfirstlane(min(max(*he.count - he.i0, 0), he.piece));          // in a scalar register: uniform in what follows from it
     const int live64 = (live + 63) & ~63;
-    int K = aux_n;
-    if (he.rows_are_k) { K = live64; Ksplit = (K / DL_BK + (int)gridDim.y - 1) / (int)gridDim.y * DL_BK; }
+    int K = aux_n, kreal = aux_s;
+    if (SWAP) { K = live64; kreal = max(live, 1); Ksplit = (K / DL_BK + (int)gridDim.y - 1) / (int)gridDim.y * DL_BK; }
     else { M = live64; tiles_m = (M + BM - 1) / BM; }
-    krange = min(Ksplit, K - z * Ksplit);
-    if (krange <= 0) krange = 0;          // the last ranges may be empty: zeros
+    krange = max(min(Ksplit, K - z * Ksplit), 0);          // the last ranges may be empty: zeros
     kbase = krange ? (size_t)z * Ksplit : 0;
+    klast = krange ? min(DL_BK, kreal - (int)kbase - (krange - DL_BK)) : min(DL_BK, kreal);
   }
   const int nb = tiles_m * tiles_n;
   // Tile walk.  The grid's x extent may be smaller than the number of tiles: workgroup b then takes the tiles b,
@@ -238,7 +241,27 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   // wave w fills rows 32w .. 32w+31 of a unit with four loads of 8 rows (8 lanes per 128-byte row) each
   const bf16_t* gA[4];
   const bf16_t* gB[4];
+  // BK_FIRST: uniform bases and 32-bit byte offsets instead.  B's unit is 64 rows (contraction) of 256 columns, 512 bytes each; wave w fills rows 8 w .. with four loads of two rows, and the
+  // 16-byte chunk c of row r sits at c ^ (2 h), h = r % 4 + 4 (bit 3 of r): the eight rows that one phase of a transpose read touches have eight different h, hence banks.
+  const char *baseA = nullptr, *baseB = nullptr;
+  uint32_t oA[4], oB[2];          // oB: loads i and i + 2 differ by four rows
+  const int brow = wave * 8 + (lane >> 5);
   auto set_ptrs = [&](int tm, int tn) {
+    if constexpr (BK_FIRST) {
+      baseA = reinterpret_cast<const char*>(A + (size_t)tm * BM * lda + kbase);
+      baseB = reinterpret_cast<const char*>(B + kbase * ldb + tn * BN);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = wave * 32 + i * 8 + (lane >> 3);
+        oA[i] = ((uint32_t)min(row, M - 1 - tm * BM) * (uint32_t)lda + ((lane & 7) ^ ((row >> 1) & 7)) * 8) * 2;
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int row = brow + 2 * q, h = (row & 3) | ((row >> 1) & 4);
+        oB[q] = ((uint32_t)row * (uint32_t)ldb + min(((lane & 31) ^ (2 * h)) * 8, he.ncols - 8 - tn * BN)) * 2;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = wave * 32 + i * 8 + (lane >> 3);
@@ -271,6 +294,34 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
 #pragma unroll
     for (int i = 0; i < 4; ++i) __builtin_amdgcn_global_load_lds(PP_GPTR(g[i] + koff), PP_LPTR(dst + i * 64), 16, 0, 0);
   };
+  // BK_FIRST: the same loads in assembly (they write no registers): the compiler, which would wait for every load into LDS that it knows of in front of a transpose read, knows of none
+  const uint32_t lds0 = (uint32_t)(uintptr_t)PP_LPTR(lds);
+  auto load_lds = [&](uint32_t dst, uint32_t off, const char* base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "memory");
+  };
+  auto issueA = [&](int s, int slot) {
+    if constexpr (BK_FIRST) {
+      const char* b = baseA + (size_t)max(min(s, ns - 1), 0) * (DL_BK * 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) load_lds(lds0 + (slot * DL_UNIT_CHUNKS + wdst + i * 64) * 16, oA[i], b);
+    } else issue(gA, s, slot);
+  };
+  auto issueB = [&](int s, int slot) {
+    if constexpr (BK_FIRST) {
+      const int sc = max(min(s, ns - 1), 0);
+      const char* b = baseB + (size_t)sc * DL_BK * ldb * 2;
+      const uint32_t dst = lds0 + (slot * DL_UNIT_CHUNKS + wdst) * 16;
+      if (sc < ns - 1 || klast == DL_BK) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_lds(dst + i * 1024, oB[i & 1], b + (size_t)(i >> 1) * 8 * ldb);
+      } else          // rows behind the last one repeat it
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = brow + 2 * i, over = row - min(row, klast - 1), back = over + (i >> 1) * -4;          // rows to go back from oB[i & 1]'s
+          load_lds(dst + i * 1024, oB[i & 1] - (uint32_t)(back * ldb * 2), b);
+        }
+    } else issue(gB, s, slot);
+  };
   auto m5 = [](int x) { return x >= DL_SLOTS ? x - DL_SLOTS : x; };
 
   const int l16 = lane & 15, lq = lane >> 4, sw = (l16 >> 1) & 7;          // row in a 16-row block, 16-byte chunk within a 64-byte K32 piece
@@ -286,7 +337,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         for (; b < nb; b += gridDim.x) {
           int m, n;
           tile_of(b, m, n);
-          if (he.redo[1 + m]) break;
+          if (__builtin_amdgcn_readfirstlane(he.redo[1 + m])) break;
         }
     return b;
   };
@@ -296,7 +347,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   }
   tile_of(vb, tm, tn);
   set_ptrs(tm, tn);
-  issue(gA, 0, 0); issue(gB, 0, 1); issue(gA, 1, 2);
+  issueA(0, 0); issueB(0, 1); issueA(1, 2);
   // Plain s_barrier (no fence): a workgroup fence would force vmcnt(0), i.e. wait for ALL loads in flight.  The only
   // LDS traffic here is DMA writes (tracked by vmcnt) and fragment reads (consumed by MFMAs before the barrier).
   __builtin_amdgcn_s_waitcnt(0x0F70 | 4);          // vmcnt(4): both units of super-step 0 have landed
@@ -325,7 +376,23 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
 #pragma unroll
     for (int i = 0; i < 4; ++i) fa[buf][i] = __builtin_bit_cast(bf16x8, pa[(half * 4 + i) * 16 * 8]);
   };
+  // BK_FIRST: lane l reads, of the four-row bands 8 (l / 16) and 8 (l / 16) + 4 of a K32 piece, row l % 16 / 4 and 8-byte piece l % 4 of the 16 columns, and receives column l % 16 of the
+  // band's four rows; blocks j of columns differ in bits 5 and 6 of the address
+  const int bh = (l16 >> 2) | ((lq & 1) << 2);
+  const uint32_t trB = (8 * lq + (l16 >> 2)) * 512 + (((wn * 4) ^ bh) << 5) + ((l16 & 3) >> 1) * 16 + (l16 & 1) * 8;
   auto readB = [&](int buf, int slot, int kk) {
+    if constexpr (BK_FIRST) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4* lptr;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t p = lds0 + slot * (DL_UNIT_CHUNKS * 16) + (trB ^ (j << 5));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(uintptr_t)(p + kk * 16384));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(uintptr_t)(p + kk * 16384 + 2048));
+        fb[buf][j] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+      return;
+    }
     const u32x4* pb = lds + slot * DL_UNIT_CHUNKS + bRow + ((4 * kk + lq) ^ sw);
 #pragma unroll
     for (int j = 0; j < 4; ++j) fb[buf][j] = __builtin_bit_cast(bf16x8, pb[j * 16 * 8]);
@@ -335,7 +402,8 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        acc[half * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[bbuf][j], fa[abuf][i], acc[half * 4 + i][j], 0, 0, 0);
+        acc[half * 4 + i][j] = SWAP ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[abuf][i], fb[bbuf][j], acc[half * 4 + i][j], 0, 0, 0)
+                                    : __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[bbuf][j], fa[abuf][i], acc[half * 4 + i][j], 0, 0, 0);
   };
   // R fragment reads behind the first MFMAs of a slice of 16 (the in-order LDS counter then never makes this slice's
   // MFMAs wait for the next slice's reads)
@@ -352,7 +420,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   readA(0, 0, 0, 0);
   for (int s = 0; s < ns; ++s) {
     const int sb = m5(sa + 1), na = m5(sa + 2), nb2 = m5(sa + 3), fa2 = m5(sa + 4);
-    issue(gB, s + 1, nb2);          // slot of A(s-1): free since the barrier that ended super-step s-1
+    issueB(s + 1, nb2);          // slot of A(s-1): free since the barrier that ended super-step s-1
     __builtin_amdgcn_sched_barrier(0);
     readA(1, sa, 0, 1);
     mm(0, 0, 0);
@@ -360,8 +428,8 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     readB(1, sb, 1);
     readA(0, sa, 1, 0);
     mm(1, 0, 1);
-    PP_DL_INTERLEAVE(1, 8);
-    issue(gA, s + 2, fa2);          // slot of B(s-1)
+    PP_DL_INTERLEAVE(1, (BK_FIRST ? 12 : 8));
+    issueA(s + 2, fa2);          // slot of B(s-1)
     __builtin_amdgcn_sched_barrier(0);
     readA(1, sa, 1, 1);
     mm(0, 1, 0);
@@ -373,7 +441,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     readB(0, nb2, 0);
     readA(0, na, 0, 0);
     mm(1, 1, 1);
-    PP_DL_INTERLEAVE(3, 8);
+    PP_DL_INTERLEAVE(3, (BK_FIRST ? 12 : 8));
     sa = na;
   }
 #undef PP_DL_INTERLEAVE
@@ -387,7 +455,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   if (has_next) {
     tile_of(vb_next, tm_next, tn_next);
     set_ptrs(tm_next, tn_next);
-    issue(gA, 0, 0); issue(gB, 0, 1); issue(gA, 1, 2);
+    issueA(0, 0); issueB(0, 1); issueA(1, 2);
   }
   __builtin_amdgcn_sched_barrier(0);
 
@@ -470,24 +538,30 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     }
     stored = true;
   } else if constexpr (EPI == EPI_HEAD_DX || EPI == EPI_HEAD_DW) {
-    // ---- fp32 patch, 32 rows at a time (as in the residual epilogue below): a lane gets 8 consecutive columns of a row
+    // ---- fp32 patch of 32 rows x 64 columns at a time (as in the residual epilogue below): a lane gets 8 consecutive columns of a row.  DX: row block pairs by the wave's 64 columns;
+    // DW, whose element r of accumulator (i, j) is row 16 j + lane % 16, column 16 i + 4 (lane / 16) + r of the wave's 64 x 128: two row block pairs by two column halves.
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    const int e16 = ln & 15, eq = ln >> 4;
 #pragma unroll
     for (int qt = 0; qt < 4; ++qt) {
 #pragma unroll
-      for (int ii = 0; ii < 2; ++ii) {
-        const int i = 2 * qt + ii, row = ii * 16 + l16;
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *reinterpret_cast<float4*>(wbase + row * 256 + (((4 * j + lq) ^ (row & 15)) << 4)) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-      }
+        for (int y = 0; y < 4; ++y) {
+          const int row = x * 16 + e16;
+          const f32x4 v = SWAP ? acc[4 * (qt & 1) + y][2 * (qt >> 1) + x] : acc[2 * qt + x][y];
+          *reinterpret_cast<float4*>(wbase + row * 256 + (((4 * y + eq) ^ (row & 15)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
+        }
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
-        const int row = 8 * it + (lane >> 3), c = lane & 7;
+        const int row = 8 * it + (ln >> 3), c = ln & 7;
         const float4 v0 = *reinterpret_cast<const float4*>(wbase + row * 256 + (((2 * c) ^ (row & 15)) << 4));
         const float4 v1 = *reinterpret_cast<const float4*>(wbase + row * 256 + (((2 * c + 1) ^ (row & 15)) << 4));
-        const int grow = m0 + wm * 128 + qt * 32 + row, gcol = n0 + wn * 64 + c * 8;
-        if (grow >= (EPI == EPI_HEAD_DX ? live : M) || gcol >= N) continue;
         float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+        const int grow = SWAP ? n0 + wn * 64 + (qt >> 1) * 32 + row - he.shift : m0 + wm * 128 + qt * 32 + row;
+        const int gcol = (SWAP ? m0 + wm * 128 + (qt & 1) * 64 : n0 + wn * 64) + c * 8, cols = SWAP ? M : N;
+        if (grow < 0 || grow >= (SWAP ? he.out_rows : live) || gcol >= cols) continue;
         size_t off;
         if constexpr (EPI == EPI_HEAD_DX) {
           const float sc = he.scale[he.i0 + grow];
@@ -504,18 +578,46 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
 #pragma unroll
               for (int e = 0; e < 8; ++e) v[e] += w[e];
             } else
-              for (int e = 0; e < 8 && gcol + e < N; ++e) v[e] += ad[e];
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (gcol + e < cols) v[e] += ad[e];
           }
         }
         if (EPI == EPI_HEAD_DW && he.out_f32) {
           float* o = reinterpret_cast<float*>(Cv) + off;
           if (he.vec) store8(o, v);
-          else for (int e = 0; e < 8 && gcol + e < N; ++e) o[e] = v[e];
+          else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (gcol + e < cols) o[e] = v[e];
         } else {
           bf16_t* o = reinterpret_cast<bf16_t*>(Cv) + off;
           if (he.vec) store8(o, v);
-          else for (int e = 0; e < 8 && gcol + e < N; ++e) o[e] = from_f32<bf16_t>(v[e]);
+          else
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (gcol + e < cols) o[e] = from_f32<bf16_t>(v[e]);
         }
+      }
+    }
+    stored = true;
+  } else if constexpr (EPI == EPI_HEAD_DW_PART) {
+    float* C = reinterpret_cast<float*>(Cv) + (size_t)z * (size_t)he.out_rows * (size_t)ldc;
+    const bool four = (ldc & 3) == 0 && (M & 3) == 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = n0 + wn * 64 + 16 * j + l16 - he.shift;
+      if (row < 0 || row >= he.out_rows) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int col = m0 + wm * 128 + 16 * i + 4 * lq;
+        if (col >= M) continue;
+        float* o = C + (size_t)row * ldc + col;
+        if (four) *reinterpret_cast<float4*>(o) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col + e < M) o[e] = acc[i][j][e];
       }
     }
     stored = true;
@@ -897,25 +999,28 @@ int k_gemm_nt_mfma(hipStream_t st, const void* A, int lda, const void* B, int ld
 
 // ---- the products of the output head's losses
 template <int EPI, bool OUT_F32>
-static int launch_head(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he) {
+static int launch_head(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int kreal, int splits, const HeadEpi& he) {
   static LdsOptIn opt_in;
   auto kern = gemm_nt_mfma_dl_kernel<EPI, OUT_F32>;
   if (!opt_in(reinterpret_cast<const void*>(kern), DL_LDS_BYTES)) return 1;
   const int tiles_m = (M + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
   const int range = (K / DL_BK + splits - 1) / splits * DL_BK;
   kern<<<dim3(splits == 1 ? dl_grid_x(tiles_m * tiles_n) : tiles_m * tiles_n, splits), 512, DL_LDS_BYTES, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, C, ldc, M, N, range, nullptr, tiles_m, tiles_n,
-                                                                                                               0, nullptr, nullptr, K, 1, he);
+                                                                                                               0, nullptr, nullptr, K, kreal, he);
   return 0;
 }
-int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he) {
-  if (M < 1 || N < 1 || K < DL_BK || K % DL_BK || (lda & 7) || (ldb & 7) || splits < 1 || (splits > 1 && epi != EPI_HEAD_PART)) return 1;
+int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int kreal, int splits, const HeadEpi& he) {
+  if (M < 1 || N < 1 || K < DL_BK || K % DL_BK || (lda & 7) || (ldb & 7) || splits < 1) return 1;
   if (((uintptr_t)A | (uintptr_t)B) & 15) return 1;
+  if (epi != EPI_HEAD_EXP && ((he.ncols & 7) || he.ncols < N || kreal < 1)) return 1;
   switch (epi) {
-    case EPI_HEAD_EXP: return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
-    case EPI_HEAD_DX: return launch_head<EPI_HEAD_DX, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
-    case EPI_HEAD_DW: return launch_head<EPI_HEAD_DW, false>(st, A, lda, B, ldb, C, ldc, M, N, K, 1, he);
-    default: return launch_head<EPI_HEAD_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, splits, he);
+    case EPI_HEAD_EXP: return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
+    case EPI_HEAD_DX: return launch_head<EPI_HEAD_DX, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
+    case EPI_HEAD_PART: return launch_head<EPI_HEAD_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, splits, he);
+    case EPI_HEAD_DW: return launch_head<EPI_HEAD_DW, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
+    case EPI_HEAD_DW_PART: return launch_head<EPI_HEAD_DW_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, splits, he);
   }
+  return 1;
 }
 
 }  // namespace pp

@@ -36,7 +36,7 @@ struct HeadPlan {
   int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
   int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
   bool grads, copy_w, own_wt, mixed;
-  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, dzt, xt, part, dwa, total;          // byte offsets
+  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, xt, part, dwa, total;          // byte offsets
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
@@ -98,7 +98,7 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.piece = std::min(std::min(p.piece, p.np), 1 << 18);          // grids of piece / 64 in y
   // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
-  p.own_wt = a.dx && !(a.wt && a.vocab % unit == 0 && a.ldwt % 8 == 0 && ((uintptr_t)a.wt & 15) == 0);
+  p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
   const long tiles_d = (a.d + 255) / 256;
   p.dx_splits = bf && a.dx ? best_splits((p.piece + 255) / 256 * tiles_d, p.vp / 64, (double)p.piece * a.d, a.part_cap) : 1;
   p.dw_splits = bf && a.dw ? best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, (double)dw_rows * a.d, a.part_cap) : 1;
@@ -122,7 +122,6 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.stats2 = take(a.top ? (size_t)p.groups * p.piece * 4 : 0);          // temperature and share are not known where the size is asked for
     p.n_redo = (p.np + p.piece - 1) / p.piece * (1 + (p.piece + 255) / 256);
     p.redo = take((size_t)p.n_redo * 4);
-    p.dzt = take(a.dw ? (size_t)(dw_rows + 8) * p.piece * es : 0);
     p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
     p.part = take(a.part_cap ? a.part_cap : std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
     p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
@@ -670,29 +669,6 @@ __global__ __launch_bounds__(256) void head_xt_kernel(const bf16_t* __restrict__
     *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
-// dst[v - v0][i] = e[i][v] for v0 <= v < v1 (v0 a multiple of 8) and the compact rows of a piece, zeros for rows behind the last one that counts
-__global__ __launch_bounds__(256) void head_et_kernel(const bf16_t* __restrict__ e, int vp, int v0, int v1, bf16_t* __restrict__ dst, int ld_dst, const int32_t* __restrict__ count, int i0, int piece) {
-  __shared__ uint16_t tile[64][72];
-  const int live = min(max(*count - i0, 0), piece), r0 = blockIdx.y * 64, c0 = v0 + blockIdx.x * 64, t = threadIdx.x;
-  if (r0 >= live) return;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = (t >> 3) + 32 * i, c8 = (t & 7) * 8;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (r0 + r < live && c0 + c8 < vp) v = *reinterpret_cast<const uint4*>(e + (size_t)(r0 + r) * vp + c0 + c8);
-    *reinterpret_cast<uint4*>(&tile[r][c8]) = v;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int c = (t >> 3) + 32 * i, r8 = (t & 7) * 8;
-    if (c0 + c >= v1) continue;
-    uint32_t w[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[r8 + 2 * k][c] | ((uint32_t)tile[r8 + 2 * k + 1][c] << 16);
-    *reinterpret_cast<uint4*>(dst + (size_t)(c0 + c - v0) * ld_dst + r0 + r8) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
 // ------------------------------------------------------------------------------------------------ few rows
 // Up to 16 rows (one block of a 16 x 16 MFMA, whichever storage type): W is streamed once for the losses, by waves that take 16 of its rows at a time from memory straight into
 // MFMA operands, and once for dX; dW is written once.  Bound by those bytes: 32000 x 2048 bf16 (131 MB) at the card's copy rate 25 us.  Logits in fp32 (16 rows of them at most),
@@ -1140,7 +1116,7 @@ static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
   }
 }
 
-static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, const void* w, int ldw, const void* wt, int ldwt, float* row_loss) {
+static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, const void* w, int ldw, float* row_loss) {
   const int dw_rows = a.dw ? a.dw_hi - a.dw_lo : 0;
   auto* rows = (int32_t*)(ws + p.rows);
   auto* count = (int32_t*)(ws + p.count);
@@ -1163,11 +1139,11 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp;
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
               !p.mixed, redo, a.tau, a.share};
-    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
+    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     he.redo = redo;
     f.again = 1;
-    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, 1, he) == 0;
+    ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     if (!e) continue;
     if (p.mixed) {
@@ -1178,33 +1154,32 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     he.scale = scale; he.rows = rows;
     if (a.dx) {
       he.vec = a.d % 8 == 0 && a.lddx % 8 == 0 && ((uintptr_t)a.dx & 15) == 0;
+      he.ncols = p.dp;          // of W: d where that is a multiple of 64, else of its padded copy
       if (p.dx_splits == 1)
-        ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, wt, ldwt, a.dx, a.lddx, m, a.d, p.vp, 1, he) == 0;
+        ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
       else {
-        ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, p.dx_splits, he) == 0;
+        ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, w, ldw, part, a.d, m, a.d, p.vp, a.vocab, p.dx_splits, he) == 0;
         head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, p.dx_splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
       }
     }
     if (a.dw) {
       const bool first = i0 == 0, last = i0 + p.piece >= a.n;
-      const int v0 = a.dw_lo & ~7;
-      bf16_t *et = (bf16_t*)(ws + p.dzt), *xt = (bf16_t*)(ws + p.xt);
+      const int v0 = a.dw_lo & ~7;          // columns of e are read in aligned groups of 8
+      bf16_t* xt = (bf16_t*)(ws + p.xt);
       head_xt_kernel<<<dim3(m / 64, p.dp / 64), 256, 0, st>>>(xp, p.dp, scale, xt, p.piece, a.d, count, i0, m);
-      head_et_kernel<<<dim3((a.dw_hi - v0 + 63) / 64, m / 64), 256, 0, st>>>(e, p.vp, v0, a.dw_hi, et, p.piece, count, i0, m);
-      et += (size_t)(a.dw_lo - v0) * p.piece;
       // the sums of several pieces are kept in fp32: in dw itself where that is float, else in the workspace until the last
       float* acc = a.dw_f32 ? (float*)a.dw : (float*)(ws + p.dwa);
       const int ldacc = a.dw_f32 ? a.lddw : a.d;
-      he.rows_are_k = 1;
+      he.shift = a.dw_lo - v0; he.out_rows = dw_rows; he.ncols = p.vp - v0;
       he.add = !first || a.dw_f32 == 2 ? acc : nullptr; he.ldadd = ldacc;
       he.out_f32 = a.dw_f32 || !last;
       void* out = he.out_f32 ? (void*)acc : a.dw;
       const int ldo = he.out_f32 ? ldacc : a.lddw;
       he.vec = a.d % 8 == 0 && ldo % 8 == 0 && (!he.add || ldacc % 8 == 0) && (((uintptr_t)out | (uintptr_t)he.add) & 15) == 0;
       if (p.dw_splits == 1)
-        ok &= k_head_gemm(st, EPI_HEAD_DW, et, p.piece, xt, p.piece, out, ldo, dw_rows, a.d, m, 1, he) == 0;
+        ok &= k_head_gemm(st, EPI_HEAD_DW, xt, p.piece, e + v0, p.vp, out, ldo, a.d, a.dw_hi - v0, m, m, 1, he) == 0;
       else {
-        ok &= k_head_gemm(st, EPI_HEAD_PART, et, p.piece, xt, p.piece, part, a.d, dw_rows, a.d, m, p.dw_splits, he) == 0;
+        ok &= k_head_gemm(st, EPI_HEAD_DW_PART, xt, p.piece, e + v0, p.vp, part, a.d, a.d, a.dw_hi - v0, m, m, p.dw_splits, he) == 0;
         if (he.out_f32) head_dw_sum_kernel<float><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (float*)out, ldo, dw_rows, a.d);
         else head_dw_sum_kernel<bf16_t><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (bf16_t*)out, ldo, dw_rows, a.d);
       }
@@ -1239,17 +1214,16 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   }
   const void* wt = a.wt;
   int ldwt = a.ldwt;
-  auto transpose = [&](const void* src, int ld_src, void* dst, int ld_dst, int r, int c) {
-    PP_H_DISPATCH(a.dtype, head_transpose_kernel<T><<<dim3((ld_dst + 63) / 64, (c + 63) / 64), 256, 0, st>>>((const T*)src, ld_src, (T*)dst, ld_dst, r, c));
-  };
-  if (p.own_wt) { transpose(a.w, a.ldw, ws + p.wt, p.vp, a.vocab, a.d); wt = ws + p.wt; ldwt = p.vp; }
-
+  if (p.own_wt) {
+    head_transpose_kernel<<<dim3((p.vp + 63) / 64, (a.d + 63) / 64), 256, 0, st>>>((const float*)a.w, a.ldw, (float*)(ws + p.wt), p.vp, a.vocab, a.d);
+    wt = ws + p.wt; ldwt = p.vp;
+  }
   if (a.n == 0 && a.dw && a.dw_f32 != 2) {
     if (a.dw_f32) head_zero_kernel<float><<<quads(dw_rows), 256, 0, st>>>((float*)a.dw, a.lddw, dw_rows, a.d);
     else PP_H_DISPATCH(a.dtype, head_zero_kernel<T><<<quads(dw_rows), 256, 0, st>>>((T*)a.dw, a.lddw, dw_rows, a.d));
   }
   bool ok = true;
-  if (a.dtype) ok = head_bf16(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
+  if (a.dtype) ok = head_bf16(st, a, p, ws, w, ldw, row_loss);
   else head_f32(st, a, p, ws, w, ldw, wt, ldwt, row_loss);
   if (a.loss) head_loss_kernel<<<1, 1024, 0, st>>>(row_loss, a.row_weight, count, a.loss, a.n);
   return ok ? 0 : 1;

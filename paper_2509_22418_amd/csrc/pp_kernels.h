@@ -19,7 +19,7 @@ struct ShadowSeg {      // one trainable row block that also lives, transposed, 
 };
 
 enum { EPI_STORE = 0, EPI_ADD_RES = 1, EPI_SWIGLU = 2, EPI_SWIGLU_BWD = 3, EPI_ROPE = 4,          // the last three: only inside k_gemm_swiglu_*_mfma / k_gemm_qkv_rope_mfma
-       EPI_HEAD_EXP = 5, EPI_HEAD_DX = 6, EPI_HEAD_DW = 7, EPI_HEAD_PART = 8 };                    // only inside k_head_gemm
+       EPI_HEAD_EXP = 5, EPI_HEAD_DX = 6, EPI_HEAD_PART = 7, EPI_HEAD_DW = 8, EPI_HEAD_DW_PART = 9 };          // only inside k_head_gemm
 
 void k_fill_f32(hipStream_t st, float* p, size_t n, float v);
 void k_rope_tables(hipStream_t st, float* cosb, float* sinb, int S, int dh, float base);
@@ -140,11 +140,10 @@ struct HeadArgs {
   int no_few;                      // ... but for the kernels of few rows, which this keeps away
 };
 // What the head's products on the bf16 matrix cores read besides their operands.  The number of rows that count is on the device only: live = clamp(*count - i0, 0, piece), and
-// whole groups of 64 rows are worked on (rows behind the last one that counts are zeros in every operand).
+// whole groups of 64 rows are worked on (rows behind the last one that counts are zeros in X and not read of e).
 struct HeadEpi {
   const int32_t* count;
   int i0, piece;
-  int rows_are_k;                  // 0: the rows are the product's rows (M = live), 1: its contraction index (K = live)
   // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and 64 columns the sum of e, the largest exponent and, where kt != 0, the sum of
   // exp2(kt (z - ref)), at [64-column group][row of the piece].
   const float* ref;
@@ -153,17 +152,23 @@ struct HeadEpi {
   float k, kt;
   int vp;
   const int32_t* redo;             // nullptr, or: [0] != 0 if any, [1 + b] != 0 if rows 256 b .. are to be done (nothing else is)
+  // the others: columns of B that can be read, a multiple of 8
+  int ncols;
   // EPI_HEAD_DX: row i of the product times scale[i] goes to row rows[i] of C
   const float* scale;
   const int32_t* rows;
-  // EPI_HEAD_DW: C = product (+ add), C float (out_f32) or bf16
+  // EPI_HEAD_DW, EPI_HEAD_DW_PART: column n of the product is row n - shift of C (out_rows of them).  DW: C = product (+ add), C float (out_f32) or bf16
+  int shift, out_rows;
   const float* add;
   int ldadd, out_f32;
   int vec;                         // DX, DW: rows of C (and add) are whole aligned groups of 8
 };
-// C = A[M x K] B[N x K]^T on 256 x 256 tiles, epi one of EPI_HEAD_*; splits > 1 (EPI_HEAD_PART): float partials [splits][M][N] to C.  M (or K) is the piece's size where it is
-// the rows that count.  Returns 0 if launched, 1 if not.
-int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int splits, const HeadEpi& he);
+// Products on 256 x 256 tiles.  EPI_HEAD_EXP: A[M x K] B[N x K]^T, K-contiguous.  The others read B [K rows x ldb] as it lies, contraction index first:
+//   EPI_HEAD_DX, EPI_HEAD_PART     C[live x N] = A[live x K] B,   K a multiple of 64; rows of B from kreal on are not read (A's columns there are zeros)
+//   EPI_HEAD_DW, EPI_HEAD_DW_PART  C[N x M] = (A[M x live] B)^T
+// M (K) is the piece's size where the rows that count are the product's rows (its contraction index).  _PART: `splits` ranges of the contraction, float partials [splits][live64][N],
+// resp. [splits][out_rows][M].  Returns 0 if launched, 1 if not.
+int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, int kreal, int splits, const HeadEpi& he);
 size_t head_bytes(const HeadArgs& a);
 bool head_is_few(const HeadArgs& a);          // whether the kernels of few rows run
 int k_head(hipStream_t st, const HeadArgs& a, char* ws);          // ws: head_bytes(a), 256-byte aligned; 0, or 1 if a kernel cannot be launched
