@@ -215,6 +215,13 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     live = __builtin_amdgcn_readfirstlane(min(max(*he.count - he.i0, 0), he.piece));          // in a scalar register: uniform in what follows from it
     const int live64 = (live + 63) & ~63;
     int K = aux_n, kreal = aux_s;
+    if constexpr (EPI == EPI_HEAD_DX) { if (__builtin_amdgcn_readfirstlane(*he.splits) != 1) return; }
+    if constexpr (EPI == EPI_HEAD_PART) {
+      const int splits = __builtin_amdgcn_readfirstlane(*he.splits);
+      if (splits == 1 || z >= splits) return;
+      Ksplit = (K / DL_BK + splits - 1) / splits * DL_BK;
+      kbase = (size_t)z * Ksplit;
+    }
     if (SWAP) { K = live64; kreal = max(live, 1); Ksplit = (K / DL_BK + (int)gridDim.y - 1) / (int)gridDim.y * DL_BK; }
     else { M = live64; tiles_m = (M + BM - 1) / BM; }
     krange = max(min(Ksplit, K - z * Ksplit), 0);          // the last ranges may be empty: zeros
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   auto tile_of = [&](int vb, int& tm, int& tn) {
     int pid = vb;
     if ((nb & 7) == 0) pid = (pid & 7) * (nb >> 3) + (pid >> 3);          // XCD k = id % 8 owns a contiguous range of tiles
-    constexpr int GROUP = 8;
+    const int GROUP = (EPI == EPI_HEAD_DX || EPI == EPI_HEAD_PART) && tiles_n <= 4 ? 4 : 8;          // few column tiles: an XCD's dozen share four row strips of e, not eight
     const int per_group = GROUP * tiles_n;
     const int group = pid / per_group;
     const int first_m = group * GROUP;
@@ -347,6 +354,12 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   }
   tile_of(vb, tm, tn);
   set_ptrs(tm, tn);
+  [[maybe_unused]] float rk[8];          // EPI_HEAD_EXP: references of the tile's rows (lane % 16 of every row block)
+  [[maybe_unused]] auto load_refs = [&](int tm) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(tm * BM + wm * 128 + 16 * i + l16, M - 1)];
+  };
+  if constexpr (EPI == EPI_HEAD_EXP) load_refs(tm);
   issueA(0, 0); issueB(0, 1); issueA(1, 2);
   // Plain s_barrier (no fence): a workgroup fence would force vmcnt(0), i.e. wait for ALL loads in flight.  The only
   // LDS traffic here is DMA writes (tracked by vmcnt) and fragment reads (consumed by MFMAs before the barrier).
@@ -462,6 +475,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   // ---- epilogue: element r of accumulator (i, j) is output row m0 + wm*128 + 16 i + lane % 16,
   //      column n0 + wn*64 + 16 j + 4 (lane / 16) + r
   bool stored = false;
+  [[maybe_unused]] int stores = 0;
   if constexpr (EPI == EPI_HEAD_EXP) {
     // ---- exponentials of a row of logits against the row's reference, their sums and the largest exponent over this wave's 64 columns; see HeadEpi
     // (the lane index is laundered as in the rotary epilogue: its addresses are formed here, not above the main loop)
@@ -479,9 +493,6 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
             for (int i = 0; i < 8; ++i) acc[i][j][r] = -INFINITY;
     }
     const int row0 = m0 + wm * 128 + e16;
-    float rk[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(row0 + 16 * i, M - 1)];
     if (he.kt != 0.f) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -512,7 +523,9 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
       t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
       if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
     }
+    if (has_next) load_refs(tm_next);
     if (C && n0 + wn * 64 < he.vp) {
+      stores = m0 + BM <= M ? 16 : 0;          // store instructions issued for certain
 #pragma unroll
       for (int hi = 0; hi < 2; ++hi) {          // turned around as in the plain store below
 #pragma unroll
@@ -853,6 +866,13 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   }
   if (!has_next) break;
   vb = vb_next; tm = tm_next; tn = tn_next;
+  if constexpr (EPI == EPI_HEAD_EXP)
+    if (stores == 16) {          // the newest 16 are stores, which need not be acknowledged: all older ones, the next tile's units among them, are done
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0x4070);          // vmcnt(16) lgkmcnt(0)
+      __builtin_amdgcn_sched_barrier(0);
+      continue;
+    }
   // the next tile's first units have landed, this wave's stores are acknowledged and its patch reads are done; the
   // barrier at the top of the loop publishes all of that before any wave refills slots 3 and 4
   __builtin_amdgcn_s_waitcnt(0x0070);

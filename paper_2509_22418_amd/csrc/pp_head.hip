@@ -40,17 +40,23 @@ struct HeadPlan {
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
-// K ranges of a product of `tiles` 256 x 256 tiles and `steps` steps of 64: the number that fills rounds of 256 workgroups best.  A tile's step takes about 0.5 us and a workgroup 4 us
-// besides; every range costs a write and a read of the M x N floats (at 4 TB/s).
-int best_splits(long tiles, long steps, double mn, size_t cap) {
-  int best = 1;
-  double cost = 0;
-  for (int s = 1; s <= 32 && steps / s >= 8; ++s) {
-    if (s > 1 && cap && s * mn * 4 > (double)cap) break;
-    const double c = (double)((tiles * s + 255) / 256) * (0.5 * ((steps + s - 1) / s) + 4) + (s > 1 ? 4 + s * mn * 8 / 4e6 : 0);
+// K ranges of a product of `tiles` 256 x 256 tiles and `steps` steps of 64: the number that fills rounds of 256 workgroups best.  In 1 / 4 us: a step takes 1.6 us, a workgroup 10 us besides (30 with
+// partial sums to write), and the launch that sums them 5 us and 0.1 us per tile and range.  (32000 x 768 over 8192 rows, 375 tiles: one range 415 us, two 397 + 73; 8192 x 768 over 32000,
+// 96 tiles: two 412 + 14, five 402 + 28; 3277 x 2048 over 32000, 104 tiles: one 572, two 345 + 26.)
+constexpr int kMaxSplits = 16;
+__host__ __device__ inline int best_splits(int tiles, int steps, int most) {
+  int best = 1, cost = 0;
+  if (tiles > 1024) return 1;
+  for (int s = 1; s <= most && steps >= 8 * s; ++s) {
+    const int c = (tiles * s + 255) / 256 * ((steps + s - 1) / s * 32 / 5 + (s > 1 ? 120 : 40)) + (s > 1 ? 20 + s * tiles * 2 / 5 : 0);
     if (s == 1 || c < cost) { best = s; cost = c; }
   }
   return best;
+}
+// ranges that fit the buffer of the partial sums
+int capped(int splits, double mn, size_t cap) {
+  while (splits > 1 && cap && splits * mn * 4 > (double)cap) --splits;
+  return splits;
 }
 
 // Few rows: threads of a workgroup side by side (8 columns each), and rows of W per workgroup such that the workgroups' partial sums of dX are kFewPartials at most.
@@ -94,14 +100,25 @@ HeadPlan plan_head(const HeadArgs& a) {
   }
   p.groups = (a.vocab + 255) / 256 * 4;
   const size_t row = (size_t)p.vp * es;
-  p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(kPieceBytes / row / 256 * 256));
+  // Every piece but the first reads and writes dW's fp32 sums: with a larger dW the pieces may be as large as that, up to 1 GiB (4096 x 4096 x 128000, in two pieces / in one: 10.5 / 9.5 ms)
+  const size_t limit = std::max(kPieceBytes, std::min(2 * kPieceBytes, (size_t)dw_rows * a.d * 4));
+  p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(limit / row / 256 * 256));
   p.piece = std::min(std::min(p.piece, p.np), 1 << 18);          // grids of piece / 64 in y
   // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
-  const long tiles_d = (a.d + 255) / 256;
-  p.dx_splits = bf && a.dx ? best_splits((p.piece + 255) / 256 * tiles_d, p.vp / 64, (double)p.piece * a.d, a.part_cap) : 1;
-  p.dw_splits = bf && a.dw ? best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, (double)dw_rows * a.d, a.part_cap) : 1;
+  // dX's ranges are decided on the device by the rows that count (head_scan_kernel): at most so many, and partial sums for the worst number of rows
+  const int tiles_d = (a.d + 255) / 256;
+  size_t dx_part = 0;
+  p.dx_splits = 1;
+  if (bf && a.dx)
+    for (int t = 1; t <= (p.piece + 255) / 256 && t * tiles_d <= 1024; ++t) {
+      const size_t rows = std::min(t * 256, p.piece);
+      const int s = capped(best_splits(t * tiles_d, p.vp / 64, kMaxSplits), (double)rows * a.d, a.part_cap);
+      p.dx_splits = std::max(p.dx_splits, s);
+      if (s > 1) dx_part = std::max(dx_part, s * rows * a.d * 4);
+    }
+  p.dw_splits = bf && a.dw ? capped(best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, kMaxSplits), (double)dw_rows * a.d, a.part_cap) : 1;
   size_t off = 0;
   auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
   p.flags = take(a.top ? p.np : 0);
@@ -120,21 +137,22 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.z = take(p.grads ? (size_t)p.piece * p.vp * es : 0);
     p.stats = take((size_t)p.groups * p.piece * 8);
     p.stats2 = take(a.top ? (size_t)p.groups * p.piece * 4 : 0);          // temperature and share are not known where the size is asked for
-    p.n_redo = (p.np + p.piece - 1) / p.piece * (1 + (p.piece + 255) / 256);
-    p.redo = take((size_t)p.n_redo * 4);
+    const int pieces = (p.np + p.piece - 1) / p.piece;
+    p.n_redo = pieces * (1 + (p.piece + 255) / 256);
+    p.redo = take((size_t)(p.n_redo + pieces) * 4);          // then the ranges of every piece's dX
     p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
-    p.part = take(a.part_cap ? a.part_cap : std::max(p.dx_splits > 1 ? (size_t)p.dx_splits * p.piece * a.d * 4 : 0, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
+    p.part = take(a.part_cap ? a.part_cap : std::max(dx_part, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
     p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
   } else {
-    // ranges of the contractions: doubled until the products have two workgroups of 32 x 32 tiles for a compute unit
+    // ranges of the contractions: doubled until the products have two workgroups of 64 x 64 tiles for a compute unit (1024 x 512, K = 8000: one range of 32 x 32 tiles 94 us)
     auto double_up = [&](long tiles, int k, int unit_k, size_t out) {
       int s = 1;
-      while (s < 32 && tiles * s < 512 && k % (2 * s * unit_k) == 0 && k / (2 * s) >= 256 && (!a.part_cap || 2 * s * out <= a.part_cap)) s *= 2;
+      while (s < 32 && tiles * s < 512 && k % (2 * s * unit_k) == 0 && k / (2 * s) >= 512 && (!a.part_cap || 2 * s * out <= a.part_cap)) s *= 2;
       return s;
     };
-    const long t32 = (a.d + 31) / 32;
-    p.dx_splits = a.dx ? double_up((p.piece + 31) / 32 * t32, p.vp, 4, (size_t)p.piece * a.d * 4) : 1;
-    p.dw_splits = a.dw ? double_up((dw_rows + 31) / 32 * t32, p.piece, 4, (size_t)dw_rows * a.d * 4) : 1;
+    const long t64 = (a.d + 63) / 64;
+    p.dx_splits = a.dx ? double_up((p.piece + 63) / 64 * t64, p.vp, 4, (size_t)p.piece * a.d * 4) : 1;
+    p.dw_splits = a.dw ? double_up((dw_rows + 63) / 64 * t64, p.piece, 4, (size_t)dw_rows * a.d * 4) : 1;
     p.z = take((size_t)p.piece * p.vp * 4);
     p.part = take(std::max({a.part_cap, a.dx ? (size_t)p.dx_splits * p.piece * a.d * 4 : (size_t)0, p.dw_splits > 1 || p.piece < a.n || a.dw_f32 == 2 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : (size_t)0}));
   }
@@ -163,7 +181,8 @@ __global__ __launch_bounds__(256) void head_flags_kernel(const int32_t* __restri
 
 // pos[t] = place of row t among the rows that count, -1 for the others; rows[i] = t; count = their number; redo cleared.  One block; 16 consecutive rows per thread.
 __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restrict__ targets, const unsigned char* __restrict__ flags, const float* __restrict__ weight, int n, int V,
-                                                         int32_t* __restrict__ pos, int32_t* __restrict__ rows, int32_t* __restrict__ count, int32_t* __restrict__ redo, int n_redo) {
+                                                         int32_t* __restrict__ pos, int32_t* __restrict__ rows, int32_t* __restrict__ count, int32_t* __restrict__ redo, int n_redo, int pieces, int piece,
+                                                         int tiles_d, int steps, int most, size_t cap, int d) {
   __shared__ int wave_sum_s[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < n_redo; i += 1024) redo[i] = 0;
@@ -224,6 +243,12 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
     base += all;
   }
   if (tid == 0) *count = base;
+  for (int i = tid; i < pieces; i += 1024) {          // every piece's ranges of dX's contraction
+    const int live = min(max(base - i * piece, 0), piece), rows = (live + 63) & ~63;
+    int s = best_splits((live + 255) / 256 * tiles_d, steps, most);
+    while (s > 1 && cap && (double)s * rows * d * 4 > (double)cap) --s;
+    redo[n_redo + i] = s;
+  }
 }
 
 // Compact, padded copy of the rows that count; zeros behind them up to the last row of the copy; the outputs of rows that are left out.  A wave per row.
@@ -994,10 +1019,11 @@ __global__ __launch_bounds__(256) void head_few_dw_kernel(HeadFew h, int cols) {
 // ------------------------------------------------------------------------------------------------ outputs
 // dx[rows[i]] = scale[i] (1 without) sum of the partials [splits][pitch][d], a wave per compact row of the piece; pitch 0: the rows that count, in whole groups of 64
 template <class T>
-__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, int pitch, const float* __restrict__ scale, T* __restrict__ dx, int lddx, int d,
+__global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const int32_t* __restrict__ splits_dev, int pitch, const float* __restrict__ scale, T* __restrict__ dx, int lddx, int d,
                                                           const int32_t* __restrict__ rows, const int32_t* __restrict__ count, int i0, int piece) {
   const int i = blockIdx.x * 4 + (threadIdx.x >> 6), live = min(max(*count - i0, 0), piece);
   if (i >= live) return;
+  if (splits_dev) { splits = *splits_dev; if (splits == 1) return; }          // then the product's own kernel wrote dx
   const size_t mn = (size_t)(pitch ? pitch : (live + 63) & ~63) * d;
   const float sc = scale ? scale[i0 + i] : 1.f;
   const int t = rows[i0 + i];
@@ -1100,7 +1126,7 @@ static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
     else head_row_kernel<1024, 0><<<m, 1024, 0, st>>>(z, g, h);
     if (a.dx) {
       k_gemm_nt_f32(st, 0, z, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, EPI_STORE, nullptr, 1, p.dx_splits, part, count, i0, m);
-      head_dx_sum_kernel<float><<<quads(m), 256, 0, st>>>(part, p.dx_splits, m, nullptr, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
+      head_dx_sum_kernel<float><<<quads(m), 256, 0, st>>>(part, p.dx_splits, nullptr, m, nullptr, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
     }
     if (a.dw) {
       // (columns too long for the kernel's offsets cannot happen: vp < 2^20 + 128)
@@ -1155,11 +1181,11 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     if (a.dx) {
       he.vec = a.d % 8 == 0 && a.lddx % 8 == 0 && ((uintptr_t)a.dx & 15) == 0;
       he.ncols = p.dp;          // of W: d where that is a multiple of 64, else of its padded copy
-      if (p.dx_splits == 1)
-        ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
-      else {
+      he.splits = (const int32_t*)(ws + p.redo) + p.n_redo + i0 / p.piece;
+      ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
+      if (p.dx_splits > 1) {
         ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, w, ldw, part, a.d, m, a.d, p.vp, a.vocab, p.dx_splits, he) == 0;
-        head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, p.dx_splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
+        head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, 0, he.splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
       }
     }
     if (a.dw) {
@@ -1203,7 +1229,8 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
     return 0;
   }
   if (a.top && a.n) head_flags_kernel<<<quads(a.n), 256, 0, st>>>(a.targets, a.ids, a.logits, a.row_weight, flags, a.n, a.vocab, a.top, a.share > 0.f);
-  head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count, (int32_t*)(ws + p.redo), p.n_redo);
+  head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count, (int32_t*)(ws + p.redo), p.n_redo,
+                                      a.dtype && a.dx ? (p.np + p.piece - 1) / p.piece : 0, p.piece, (a.d + 255) / 256, p.vp / 64, p.dx_splits, a.part_cap, a.d);
   if (a.dtype == 0)
     head_gather_kernel<float><<<quads(p.np), 256, 0, st>>>((const float*)a.x, a.ldx, (float*)xc, p.dp, a.d, pos, count, a.n, p.np, (float*)a.dx, a.lddx, row_loss, a.row_lse);
   const void* w = a.w;

@@ -154,6 +154,7 @@ struct HeadEpi {
   const int32_t* redo;             // nullptr, or: [0] != 0 if any, [1 + b] != 0 if rows 256 b .. are to be done (nothing else is)
   // the others: columns of B that can be read, a multiple of 8
   int ncols;
+  const int32_t* splits;           // EPI_HEAD_DX, EPI_HEAD_PART: ranges of the contraction, decided on the device where the rows are counted: DX runs where that is 1, PART where it is more
   // EPI_HEAD_DX: row i of the product times scale[i] goes to row rows[i] of C
   const float* scale;
   const int32_t* rows;
