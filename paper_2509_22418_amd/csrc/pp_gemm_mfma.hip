@@ -506,47 +506,54 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         if (eq == 0 && row0 + 16 * i < M) he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = s2;
       }
     }
+    // sum / maximum over the four lanes that hold a row's columns: row swaps in registers instead of trips through LDS
+    auto swap16 = [](float v) { return __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
+    auto swap32 = [](float v) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
+    const bool keep = C && n0 + wn * 64 < he.vp;
+    stores = !keep || m0 + BM <= M ? 8 : 0;          // vector memory instructions issued for certain behind everything else: the second half's stores, or the next tile's references
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float off = -rk[i] * he.k;
-      float s = 0.f, t = -INFINITY;
+    for (int hi = 0; hi < 2; ++hi) {          // half of the rows at a time: the first half's stores leave while the second's exponentials are formed
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int ii = 0; ii < 4; ++ii) {
+        const int i = 4 * hi + ii;
+        const float off = -rk[i] * he.k;
+        float s = 0.f, t = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float y = fmaf(acc[i][j][r], he.k, off);
-          t = fmaxf(t, y);
-          acc[i][j][r] = __builtin_amdgcn_exp2f(y);
-          s += acc[i][j][r];
-        }
-      s += __shfl_xor(s, 16, 64); s += __shfl_xor(s, 32, 64);
-      t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
-      if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
-    }
-    if (has_next) load_refs(tm_next);
-    if (C && n0 + wn * 64 < he.vp) {
-      stores = m0 + BM <= M ? 16 : 0;          // store instructions issued for certain
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int hi = 0; hi < 2; ++hi) {          // turned around as in the plain store below
-#pragma unroll
-        for (int ii = 0; ii < 4; ++ii) {
-          const int i = 4 * hi + ii, row = ii * 16 + e16, sw2 = (row >> 1) & 7;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int q = 4 * j + eq;
-            uint2 w;
-            w.x = f32x2_to_bf16x2(acc[i][j][0], acc[i][j][1]);
-            w.y = f32x2_to_bf16x2(acc[i][j][2], acc[i][j][3]);
-            *reinterpret_cast<uint2*>(wbase + row * 128 + (((q >> 1) ^ sw2) << 4) + (q & 1) * 8) = w;
+          for (int r = 0; r < 4; ++r) {
+            const float y = fmaf(acc[i][j][r], he.k, off);
+            t = fmaxf(t, y);
+            acc[i][j][r] = __builtin_amdgcn_exp2f(y);
+            s += acc[i][j][r];
           }
-        }
+        const auto s16 = swap16(s), t16 = swap16(t);
+        s = __uint_as_float(s16[0]) + __uint_as_float(s16[1]); t = fmaxf(__uint_as_float(t16[0]), __uint_as_float(t16[1]));
+        const auto s32 = swap32(s), t32 = swap32(t);
+        s = __uint_as_float(s32[0]) + __uint_as_float(s32[1]); t = fmaxf(__uint_as_float(t32[0]), __uint_as_float(t32[1]));
+        if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
+      }
+      if (hi == 1 && has_next) load_refs(tm_next);
+      if (!keep) continue;
+      // turned around as in the plain store below
 #pragma unroll
-        for (int it = 0; it < 8; ++it) {
-          const int row = 8 * it + (ln >> 3), c = ln & 7;
-          const uint4 v = *reinterpret_cast<const uint4*>(wbase + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
-          const int grow = m0 + wm * 128 + hi * 64 + row;
-          if (grow < M) *reinterpret_cast<uint4*>(C + (size_t)grow * ldc + n0 + wn * 64 + c * 8) = v;
+      for (int ii = 0; ii < 4; ++ii) {
+        const int i = 4 * hi + ii, row = ii * 16 + e16, sw2 = (row >> 1) & 7;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int q = 4 * j + eq;
+          uint2 w;
+          w.x = f32x2_to_bf16x2(acc[i][j][0], acc[i][j][1]);
+          w.y = f32x2_to_bf16x2(acc[i][j][2], acc[i][j][3]);
+          *reinterpret_cast<uint2*>(wbase + row * 128 + (((q >> 1) ^ sw2) << 4) + (q & 1) * 8) = w;
         }
+      }
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        const int row = 8 * it + (ln >> 3), c = ln & 7;
+        const uint4 v = *reinterpret_cast<const uint4*>(wbase + row * 128 + ((c ^ ((row >> 1) & 7)) << 4));
+        const int grow = m0 + wm * 128 + hi * 64 + row;
+        if (grow < M) *reinterpret_cast<uint4*>(C + (size_t)grow * ldc + n0 + wn * 64 + c * 8) = v;
       }
     }
     stored = true;
@@ -867,9 +874,9 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   if (!has_next) break;
   vb = vb_next; tm = tm_next; tn = tn_next;
   if constexpr (EPI == EPI_HEAD_EXP)
-    if (stores == 16) {          // the newest 16 are stores, which need not be acknowledged: all older ones, the next tile's units among them, are done
+    if (stores == 8) {          // the newest 8 need not be done: all older ones, the next tile's units among them, are
       __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(0x4070);          // vmcnt(16) lgkmcnt(0)
+      __builtin_amdgcn_s_waitcnt(0x0070 | 8);          // vmcnt(8) lgkmcnt(0)
       __builtin_amdgcn_sched_barrier(0);
       continue;
     }
@@ -1034,7 +1041,9 @@ int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, 
   if (((uintptr_t)A | (uintptr_t)B) & 15) return 1;
   if (epi != EPI_HEAD_EXP && ((he.ncols & 7) || he.ncols < N || kreal < 1)) return 1;
   switch (epi) {
-    case EPI_HEAD_EXP: return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
+    case EPI_HEAD_EXP:
+      if (he.tile) return k_head_exp_ring(st, A, lda, B, ldb, C, ldc, M, N, K, he);
+      return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
     case EPI_HEAD_DX: return launch_head<EPI_HEAD_DX, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
     case EPI_HEAD_PART: return launch_head<EPI_HEAD_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, splits, he);
     case EPI_HEAD_DW: return launch_head<EPI_HEAD_DW, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);

@@ -47,7 +47,7 @@ struct RingFused {          // operands of the fused epilogues (ring_fused below
 };
 template <int EPI, int BM, int BN, int WM, int WN, int NS, bool WHOLE, bool TOUCH>
 __global__ __launch_bounds__(64 * WM * WN, WHOLE ? 1 : NS == 2 ? 4 : 2) void gemm_nt_ring_kernel(const bf16_t* __restrict__ A, int lda, const bf16_t* __restrict__ B, int ldb,
-                                                                         bf16_t* C, int ldc, int M, int N, int K, const bf16_t* R, int tiles_m, int tiles_n, int vec, int touch, RingFused fu) {
+                                                                         bf16_t* C, int ldc, int M, int N, int K, const bf16_t* R, int tiles_m, int tiles_n, int vec, int touch, RingFused fu, HeadEpi he) {
   constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MI = TM / 16, NJ = TN / 16, FR = MI + NJ;
   constexpr int STAGE = (BM + BN) * 128, LPW = (BM + BN) / 8 / NW;          // bytes of a stage; wave-loads (8 rows) per wave
   constexpr int PITCH = TN * 4 + 16;                                         // epilogue patch: bytes per row
@@ -66,6 +66,11 @@ __global__ __launch_bounds__(64 * WM * WN, WHOLE ? 1 : NS == 2 ? 4 : 2) void gem
   const int in_group = pid - group * per_group;
   const int m0 = (first_m + in_group % gsz) * BM, n0 = (in_group / gsz) * BN;
   const int ns = K / 64;
+  if constexpr (EPI == EPI_HEAD_EXP) {          // rows that count; a second launch does the flagged blocks of 256 rows
+    if (he.redo && (he.redo[0] == 0 || he.redo[1 + m0 / 256] == 0)) return;
+    M = (__builtin_amdgcn_readfirstlane(min(max(*he.count - he.i0, 0), he.piece)) + 63) & ~63;
+    if (m0 >= M) return;
+  }
 
   // ---- fill: wave-load q of a stage is rows 8 q .. 8 q + 7 of the stacked A and B panels; wave w has q = w, w + NW, ...
   const bf16_t* g[LPW];
@@ -231,6 +236,37 @@ __global__ __launch_bounds__(64 * WM * WN, WHOLE ? 1 : NS == 2 ? 4 : 2) void gem
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         *reinterpret_cast<float4*>(patch + (i * 16 + l16) * PITCH + j * 64 + lq * 16) = make_float4(acc[2 * p + i][j][0], acc[2 * p + i][j][1], acc[2 * p + i][j][2], acc[2 * p + i][j][3]);
+    if constexpr (EPI == EPI_HEAD_EXP) {
+      // exponentials of 8 columns of a row against its reference (see HeadEpi); PR lanes side by side have the row's TN columns
+      static_assert(EPI != EPI_HEAD_EXP || PR == 4, "a row's lanes");
+#pragma unroll
+      for (int it = 0; it < NP; ++it) {
+        const int idx = it * 64 + lane, row = idx / PR, c = idx % PR;
+        const int grow = m0 + wm * TM + p * 32 + row, gcol = n0 + wn * TN + c * 8;
+        float z[8], s = 0.f, s2 = 0.f, t = -INFINITY;
+        load8(reinterpret_cast<const float*>(patch + row * PITCH + c * 32), z);
+        const float ref = he.ref[he.i0 + min(grow, M - 1)], off = -ref * he.k, off2 = -ref * he.kt;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool in = gcol + e < N;
+          const float y = in ? fmaf(z[e], he.k, off) : -INFINITY;
+          if (he.kt != 0.f) s2 += in ? __builtin_amdgcn_exp2f(fmaf(z[e], he.kt, off2)) : 0.f;
+          t = fmaxf(t, y);
+          z[e] = __builtin_amdgcn_exp2f(y);
+          s += z[e];
+        }
+#pragma unroll
+        for (int o = 1; o < PR; o <<= 1) { s += __shfl_xor(s, o, 64); t = fmaxf(t, __shfl_xor(t, o, 64)); s2 += __shfl_xor(s2, o, 64); }
+        if (grow >= M) continue;
+        if (C && gcol < he.vp) store8(C + (size_t)grow * ldc + gcol, z);
+        if (c == 0) {
+          const size_t at = (size_t)((n0 + wn * TN) / TN) * he.piece + grow;
+          he.stats[at] = make_float2(s, t);
+          if (he.kt != 0.f) he.stats2[at] = s2;
+        }
+      }
+      continue;
+    }
     if constexpr (EPI == EPI_SWIGLU || EPI == EPI_ROPE) {
       if (EPI == EPI_SWIGLU || n0 < fu.rot) {          // pairs: 8 first members and their partners TN / 2 columns further on
         constexpr int HP = TN / 16;
@@ -336,7 +372,7 @@ static int launch_ring(hipStream_t st, const void* A, int lda, const void* B, in
   const int vec = ((N | ldc) & 7) == 0 && (al & 15) == 0 ? 8 : ((N | ldc) & 3) == 0 && (al & 7) == 0 ? 4 : 1;
   const long threads = (long)tiles_m * tiles_n * 64 * WM * WN, pieces = (long)N * (K / 64);
   const int touch = TOUCH ? (int)std::min(4l, (pieces + threads - 1) / threads) : 0;          // words of B per thread
-  kern<<<dim3(tiles_m * tiles_n), 64 * WM * WN, LDS, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, (bf16_t*)C, ldc, M, N, K, (const bf16_t*)R, tiles_m, tiles_n, vec, touch, RingFused{});
+  kern<<<dim3(tiles_m * tiles_n), 64 * WM * WN, LDS, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, (bf16_t*)C, ldc, M, N, K, (const bf16_t*)R, tiles_m, tiles_n, vec, touch, RingFused{}, HeadEpi{});
   return 0;
 }
 // The tiles, with what was measured of each (ns): one K step of 64 when 1, 2, .. workgroups share a compute unit and every unit has one; the part of
@@ -404,7 +440,7 @@ static int launch_fused(hipStream_t st, const void* A, int lda, const void* B, i
   static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) == hipSuccess;
   if (!ok) return 1;
   const int tiles_m = (M + 127) / 128;
-  kern<<<dim3(tiles_m * tiles_n), 512, LDS, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, (bf16_t*)C, ldc, M, N, K, (const bf16_t*)R, tiles_m, tiles_n, 8, 0, fu);
+  kern<<<dim3(tiles_m * tiles_n), 512, LDS, st>>>((const bf16_t*)A, lda, (const bf16_t*)B, ldb, (bf16_t*)C, ldc, M, N, K, (const bf16_t*)R, tiles_m, tiles_n, 8, 0, fu, HeadEpi{});
   return 0;
 }
 int k_gemm_swiglu_fwd_ring(hipStream_t st, const void* X, int ldx, const void* Wgu, int ldw, void* gu, void* a, int M, int F, int K) {
@@ -424,6 +460,31 @@ int k_gemm_nt_ring(hipStream_t st, const void* A, int lda, const void* B, int ld
   if (M < 1 || N < 1 || K < 64 || K % 64 || (lda & 7) || (ldb & 7) || (((uintptr_t)A | (uintptr_t)B) & 15)) return 1;
   if (epi == EPI_ADD_RES) return R ? dispatch_ring<EPI_ADD_RES>(st, A, lda, B, ldb, C, ldc, M, N, K, R) : 1;
   return epi == EPI_STORE ? dispatch_ring<EPI_STORE>(st, A, lda, B, ldb, C, ldc, M, N, K, nullptr) : 1;
+}
+
+// ---- exponentials of the output head's logits on 64 x 64 and 128 x 128 tiles
+// Which: by what the parts of a launch take (kTiles' steps; an epilogue of 3 / 5 us; a 256 x 256 tile 1.6 us a step and 8 us besides), for rounds of 256 units.
+int head_exp_ring(int M, int N, int K) {
+  const int steps = K / 64;
+  auto tiles = [&](int b) { return (long)((M + b - 1) / b) * ((N + b - 1) / b); };
+  const long big = (tiles(256) + 255) / 256 * (1600l * steps + 8000);
+  const long t128 = (tiles(128) + 255) / 256 * (493l * steps + 5000), t64 = (tiles(64) + 511) / 512 * (tiles(64) > 256 ? 371l * steps + 4000 : 216l * steps + 3000);
+  if (std::min(t128, t64) >= big) return 0;
+  return t64 < t128 ? 64 : 128;
+}
+template <int B, int WM, int WN, bool WHOLE>
+static int launch_exp(hipStream_t st, const void* A, int lda, const void* Bp, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he) {
+  constexpr int NS = 4, LDS = NS * 2 * B * 128;
+  auto kern = gemm_nt_ring_kernel<EPI_HEAD_EXP, B, B, WM, WN, NS, WHOLE, false>;
+  static const bool ok = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS) == hipSuccess;
+  if (!ok) return 1;
+  const int tiles_m = (M + B - 1) / B, tiles_n = (N + B - 1) / B;
+  kern<<<dim3(tiles_m * tiles_n), 64 * WM * WN, LDS, st>>>((const bf16_t*)A, lda, (const bf16_t*)Bp, ldb, (bf16_t*)C, ldc, M, N, K, nullptr, tiles_m, tiles_n, 8, 0, RingFused{}, he);
+  return 0;
+}
+int k_head_exp_ring(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he) {
+  if (he.tile == 128) return launch_exp<128, 2, 4, false>(st, A, lda, B, ldb, C, ldc, M, N, K, he);
+  return he.tile == 64 ? launch_exp<64, 2, 2, true>(st, A, lda, B, ldb, C, ldc, M, N, K, he) : 1;
 }
 
 }  // namespace pp

@@ -33,9 +33,9 @@ namespace {
 constexpr int kTopMax = 128;          // entries per row (PP_HEAD_TOP_MAX)
 constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
-  int dp, vp, np, piece, groups;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, 64-column groups of the first product's tiles
+  int dp, vp, np, piece, groups, exp_tile;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, column groups of the first product's partial sums, its tile (0: 256)
   int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
-  bool grads, copy_w, own_wt, mixed;
+  bool grads, copy_w, own_wt, mixed, dx_whole;
   size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, xt, part, dwa, total;          // byte offsets
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
@@ -43,7 +43,7 @@ int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 // K ranges of a product of `tiles` 256 x 256 tiles and `steps` steps of 64: the number that fills rounds of 256 workgroups best.  In 1 / 4 us: a step takes 1.6 us, a workgroup 10 us besides (30 with
 // partial sums to write), and the launch that sums them 5 us and 0.1 us per tile and range.  (32000 x 768 over 8192 rows, 375 tiles: one range 415 us, two 397 + 73; 8192 x 768 over 32000,
 // 96 tiles: two 412 + 14, five 402 + 28; 3277 x 2048 over 32000, 104 tiles: one 572, two 345 + 26.)
-constexpr int kMaxSplits = 16;
+constexpr int kMaxSplits = 32;
 __host__ __device__ inline int best_splits(int tiles, int steps, int most) {
   int best = 1, cost = 0;
   if (tiles > 1024) return 1;
@@ -98,12 +98,15 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.total = off;
     return p;
   }
-  p.groups = (a.vocab + 255) / 256 * 4;
   const size_t row = (size_t)p.vp * es;
   // Every piece but the first reads and writes dW's fp32 sums: with a larger dW the pieces may be as large as that, up to 1 GiB (4096 x 4096 x 128000, in two pieces / in one: 10.5 / 9.5 ms)
   const size_t limit = std::max(kPieceBytes, std::min(2 * kPieceBytes, (size_t)dw_rows * a.d * 4));
   p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(limit / row / 256 * 256));
   p.piece = std::min(std::min(p.piece, p.np), 1 << 18);          // grids of piece / 64 in y
+  // columns that one partial sum of a row covers, by the tiles of the first product; the last piece, which may be smaller, takes the tiles of the others
+  p.exp_tile = bf ? head_exp_ring(p.piece, a.vocab, p.dp) : 0;
+  const int wide = p.exp_tile ? p.exp_tile : 256;
+  p.groups = (a.vocab + wide - 1) / wide * (wide / (p.exp_tile ? 32 : 64));
   // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
@@ -111,11 +114,13 @@ HeadPlan plan_head(const HeadArgs& a) {
   const int tiles_d = (a.d + 255) / 256;
   size_t dx_part = 0;
   p.dx_splits = 1;
+  p.dx_whole = (p.piece + 255) / 256 * tiles_d > 1024;          // whether any number of rows takes one range
   if (bf && a.dx)
     for (int t = 1; t <= (p.piece + 255) / 256 && t * tiles_d <= 1024; ++t) {
       const size_t rows = std::min(t * 256, p.piece);
       const int s = capped(best_splits(t * tiles_d, p.vp / 64, kMaxSplits), (double)rows * a.d, a.part_cap);
       p.dx_splits = std::max(p.dx_splits, s);
+      p.dx_whole |= s == 1;
       if (s > 1) dx_part = std::max(dx_part, s * rows * a.d * 4);
     }
   p.dw_splits = bf && a.dw ? capped(best_splits((dw_rows + 255) / 256 * tiles_d, p.piece / 64, kMaxSplits), (double)dw_rows * a.d, a.part_cap) : 1;
@@ -135,8 +140,9 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.coef = take(a.top ? (size_t)p.piece * 8 : 0);
     p.zsel = take((size_t)p.np * (a.top + 1) * 4);
     p.z = take(p.grads ? (size_t)p.piece * p.vp * es : 0);
-    p.stats = take((size_t)p.groups * p.piece * 8);
-    p.stats2 = take(a.top ? (size_t)p.groups * p.piece * 4 : 0);          // temperature and share are not known where the size is asked for
+    const size_t sums = (size_t)(a.part_cap ? (a.vocab + 255) / 256 * 8 : p.groups) * p.piece;          // part_cap: for either tile, so that fewer rows never need more
+    p.stats = take(sums * 8);
+    p.stats2 = take(a.top ? sums * 4 : 0);          // temperature and share are not known where the size is asked for
     const int pieces = (p.np + p.piece - 1) / p.piece;
     p.n_redo = pieces * (1 + (p.piece + 255) / 256);
     p.redo = take((size_t)(p.n_redo + pieces) * 4);          // then the ranges of every piece's dX
@@ -480,7 +486,7 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   if (lane == 0 && blockIdx.y == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
 }
 
-// A block per 16 compact rows of the piece: sums over the 64-column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
+// A block per 16 compact rows of the piece: sums over the column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
 // entries.  `again`: only rows of blocks that were done again.
 struct HeadFin {
   const float2* stats;
@@ -1162,7 +1168,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     const bf16_t* xp = xc + (size_t)i0 * p.dp;
     auto* redo = (int32_t*)(ws + p.redo) + (size_t)(i0 / p.piece) * (1 + (p.piece + 255) / 256);
     HeadEpi he{};
-    he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp;
+    he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp; he.tile = p.exp_tile;
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
               !p.mixed, redo, a.tau, a.share};
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
@@ -1182,7 +1188,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
       he.vec = a.d % 8 == 0 && a.lddx % 8 == 0 && ((uintptr_t)a.dx & 15) == 0;
       he.ncols = p.dp;          // of W: d where that is a multiple of 64, else of its padded copy
       he.splits = (const int32_t*)(ws + p.redo) + p.n_redo + i0 / p.piece;
-      ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
+      if (p.dx_whole) ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
       if (p.dx_splits > 1) {
         ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, w, ldw, part, a.d, m, a.d, p.vp, a.vocab, p.dx_splits, he) == 0;
         head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, 0, he.splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);

@@ -144,12 +144,13 @@ struct HeadArgs {
 struct HeadEpi {
   const int32_t* count;
   int i0, piece;
-  // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and 64 columns the sum of e, the largest exponent and, where kt != 0, the sum of
-  // exp2(kt (z - ref)), at [64-column group][row of the piece].
+  // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and group of columns the sum of e, the largest exponent and, where kt != 0,
+  // the sum of exp2(kt (z - ref)), at [group][row of the piece].
   const float* ref;
   float2* stats;
   float* stats2;
   float k, kt;
+  int tile;                        // 0: 256 x 256 tiles, groups of 64 columns; 128, 64: the smaller-tile GEMM's, groups of 32
   int vp;
   const int32_t* redo;             // nullptr, or: [0] != 0 if any, [1 + b] != 0 if rows 256 b .. are to be done (nothing else is)
   // the others: columns of B that can be read, a multiple of 8
@@ -164,6 +165,9 @@ struct HeadEpi {
   int ldadd, out_f32;
   int vec;                         // DX, DW: rows of C (and add) are whole aligned groups of 8
 };
+// The exponentials on the smaller-tile GEMM's tiles (he.tile); head_exp_ring: which pay for M rows at most, 0: none
+int head_exp_ring(int M, int N, int K);
+int k_head_exp_ring(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he);
 // Products on 256 x 256 tiles.  EPI_HEAD_EXP: A[M x K] B[N x K]^T, K-contiguous.  The others read B [K rows x ldb] as it lies, contraction index first:
 //   EPI_HEAD_DX, EPI_HEAD_PART     C[live x N] = A[live x K] B,   K a multiple of 64; rows of B from kreal on are not read (A's columns there are zeros)
 //   EPI_HEAD_DW, EPI_HEAD_DW_PART  C[N x M] = (A[M x live] B)^T
