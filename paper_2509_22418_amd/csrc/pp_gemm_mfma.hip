@@ -208,10 +208,11 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   size_t kbase = (size_t)z * Ksplit;
   // Head: BK_FIRST, B lies contraction index first and its fragments are gathered by LDS transpose reads; SWAP, the product is stored transposed, and the MFMAs' operands are
   // exchanged so that a lane holds four consecutive elements of a row of what is stored.
-  constexpr bool BK_FIRST = EPI >= EPI_HEAD_DX, SWAP = EPI == EPI_HEAD_DW || EPI == EPI_HEAD_DW_PART;
+  constexpr bool EXP = EPI == EPI_HEAD_EXP || EPI == EPI_HEAD_EXP_PICK, PICK = EPI == EPI_HEAD_EXP_PICK;
+  constexpr bool BK_FIRST = EPI >= EPI_HEAD_DX && !EXP, SWAP = EPI == EPI_HEAD_DW || EPI == EPI_HEAD_DW_PART;
   int live = 0, klast = 0;          // klast: rows of B in the last step
   if constexpr (EPI >= EPI_HEAD_EXP) {
-    if (EPI == EPI_HEAD_EXP && he.redo && he.redo[0] == 0) return;
+    if (EXP && he.redo && he.redo[0] == 0) return;
     live = __builtin_amdgcn_readfirstlane(min(max(*he.count - he.i0, 0), he.piece));          // in a scalar register: uniform in what follows from it
     const int live64 = (live + 63) & ~63;
     int K = aux_n, kreal = aux_s;
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
 
   int vb = blockIdx.x, tm, tn;
   auto wanted = [&](int b) {          // the first tile from b on that is to be done
-    if constexpr (EPI == EPI_HEAD_EXP)
+    if constexpr (EXP)
       if (he.redo)
         for (; b < nb; b += gridDim.x) {
           int m, n;
@@ -359,13 +360,28 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
 #pragma unroll
     for (int i = 0; i < 8; ++i) rk[i] = he.ref[he.i0 + min(tm * BM + wm * 128 + 16 * i + l16, M - 1)];
   };
-  if constexpr (EPI == EPI_HEAD_EXP) load_refs(tm);
+  [[maybe_unused]] int lo = 0, hi_ = 0;          // PICK: this wave's list of wanted entries; the first 64 of it are requested ahead of the main loop
+  [[maybe_unused]] auto load_bounds = [&](int tm, int tn) {
+    lo = hi_ = 0;
+    if (tm * BM + wm * 128 >= M) return;          // there are lists for the 128-row halves that have rows
+    const int32_t* o = he.offs + (size_t)(tm * 2 + wm) * (tiles_n * 4 + 1) + tn * 4 + wn;
+    lo = o[0]; hi_ = o[1];
+  };
+  if constexpr (EXP) {
+    load_refs(tm);
+    if constexpr (PICK) load_bounds(tm, tn);
+  }
   issueA(0, 0); issueB(0, 1); issueA(1, 2);
   // Plain s_barrier (no fence): a workgroup fence would force vmcnt(0), i.e. wait for ALL loads in flight.  The only
   // LDS traffic here is DMA writes (tracked by vmcnt) and fragment reads (consumed by MFMAs before the barrier).
   __builtin_amdgcn_s_waitcnt(0x0F70 | 4);          // vmcnt(4): both units of super-step 0 have landed
   for (;;) {
   const int m0 = tm * BM, n0 = tn * BN;
+  [[maybe_unused]] int ent = 0;
+  if constexpr (PICK) {
+      lo = __builtin_amdgcn_readfirstlane(lo); hi_ = __builtin_amdgcn_readfirstlane(hi_);
+      if (lo + lane < hi_) ent = he.list[(size_t)(tm * 2 + wm) * 128 * he.top + lo + lane];
+    }
   __builtin_amdgcn_s_barrier();
 
   // 16 x 16 x 32 MFMAs: on non-trivial operand data the matrix pipe is power-limited, and this shape sustains about
@@ -476,7 +492,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   //      column n0 + wn*64 + 16 j + 4 (lane / 16) + r
   bool stored = false;
   [[maybe_unused]] int stores = 0;
-  if constexpr (EPI == EPI_HEAD_EXP) {
+  if constexpr (EXP) {
     // ---- exponentials of a row of logits against the row's reference, their sums and the largest exponent over this wave's 64 columns; see HeadEpi
     // (the lane index is laundered as in the rotary epilogue: its addresses are formed here, not above the main loop)
     int ln = lane;
@@ -493,6 +509,26 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
             for (int i = 0; i < 8; ++i) acc[i][j][r] = -INFINITY;
     }
     const int row0 = m0 + wm * 128 + e16;
+    if (PICK && lo < hi_) {          // wanted logits, by way of the wave's patch: 32 rows of floats at a time (16-byte piece p of row r at p ^ (r & 15))
+      const int32_t* list = he.list + (size_t)(tm * 2 + wm) * 128 * he.top;
+      const size_t base = (size_t)(he.i0 + m0 + wm * 128);
+#pragma unroll
+      for (int qt = 0; qt < 4; ++qt) {
+        if (hi_ - lo <= 64 && !__ballot(lo + ln < hi_ && ((ent >> 5) & 3) == qt)) continue;
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int row = x * 16 + e16;
+            *reinterpret_cast<float4*>(wbase + row * 256 + (((4 * j + eq) ^ (row & 15)) << 4)) = make_float4(acc[2 * qt + x][j][0], acc[2 * qt + x][j][1], acc[2 * qt + x][j][2], acc[2 * qt + x][j][3]);
+          }
+        for (int at = lo + ln; at < hi_; at += 64) {
+          const int en = at < lo + 64 ? ent : list[at], row = en & 127, c = (en >> 7) & 63;
+          if ((row >> 5) == qt)
+            he.zsel[(base + row) * (he.top + 1) + (en >> 13)] = *reinterpret_cast<const float*>(wbase + (row & 31) * 256 + (((c >> 2) ^ (row & 15)) << 4) + (c & 3) * 4);
+        }
+      }
+    }
     if (he.kt != 0.f) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -533,7 +569,10 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         s = __uint_as_float(s32[0]) + __uint_as_float(s32[1]); t = fmaxf(__uint_as_float(t32[0]), __uint_as_float(t32[1]));
         if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
       }
-      if (hi == 1 && has_next) load_refs(tm_next);
+      if (hi == 1 && has_next) {
+        if constexpr (PICK) load_bounds(tm_next, tn_next);
+        load_refs(tm_next);
+      }
       if (!keep) continue;
       // turned around as in the plain store below
 #pragma unroll
@@ -873,7 +912,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   }
   if (!has_next) break;
   vb = vb_next; tm = tm_next; tn = tn_next;
-  if constexpr (EPI == EPI_HEAD_EXP)
+  if constexpr (EXP)
     if (stores == 8) {          // the newest 8 need not be done: all older ones, the next tile's units among them, are
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_waitcnt(0x0070 | 8);          // vmcnt(8) lgkmcnt(0)
@@ -1043,6 +1082,7 @@ int k_head_gemm(hipStream_t st, int epi, const void* A, int lda, const void* B, 
   switch (epi) {
     case EPI_HEAD_EXP:
       if (he.tile) return k_head_exp_ring(st, A, lda, B, ldb, C, ldc, M, N, K, he);
+      if (he.offs) return launch_head<EPI_HEAD_EXP_PICK, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
       return launch_head<EPI_HEAD_EXP, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
     case EPI_HEAD_DX: return launch_head<EPI_HEAD_DX, false>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, 1, he);
     case EPI_HEAD_PART: return launch_head<EPI_HEAD_PART, true>(st, A, lda, B, ldb, C, ldc, M, N, K, kreal, splits, he);

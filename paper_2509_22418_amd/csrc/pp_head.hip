@@ -35,8 +35,8 @@ constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
   int dp, vp, np, piece, groups, exp_tile;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, column groups of the first product's partial sums, its tile (0: 256)
   int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
-  bool grads, copy_w, own_wt, mixed, dx_whole;
-  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, xt, part, dwa, total;          // byte offsets
+  bool grads, copy_w, own_wt, mixed, dx_whole, pick;          // pick: the first product picks the entries' logits
+  size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, offs, list, xt, part, dwa, total;          // byte offsets
 };
 int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 
@@ -107,6 +107,11 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.exp_tile = bf ? head_exp_ring(p.piece, a.vocab, p.dp) : 0;
   const int wide = p.exp_tile ? p.exp_tile : 256;
   p.groups = (a.vocab + wide - 1) / wide * (wide / (p.exp_tile ? 32 : 64));
+  // Logits of the teacher's entries: by dot products (head_ref_kernel), a row of W each (7 TB/s, out of the last-level cache), or picked from the first product's accumulators (12 us for the lists and
+  // about 1.2 us for each round of tiles: 8192 x 2048 x 32000 with 64 entries a row 315 us / 50 us).
+  const double rounds = (double)((p.piece + 255) / 256) * ((a.vocab + 255) / 256) / 256;
+  p.pick = bf && a.top && !p.exp_tile && a.vocab <= 1 << 19 &&          // (the lists' counters fit 32 KB of LDS)
+           (double)p.piece * a.top * p.dp * 2 / 7e6 > 15 + 1.2 * rounds;
   // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
@@ -146,6 +151,9 @@ HeadPlan plan_head(const HeadArgs& a) {
     const int pieces = (p.np + p.piece - 1) / p.piece;
     p.n_redo = pieces * (1 + (p.piece + 255) / 256);
     p.redo = take((size_t)(p.n_redo + pieces) * 4);          // then the ranges of every piece's dX
+    const bool room = p.pick || (a.part_cap && a.top);          // part_cap: fewer entries or rows never need more
+    p.offs = take(room ? (size_t)(p.piece + 127) / 128 * ((a.vocab + 255) / 256 * 4 + 1) * 4 : 0);
+    p.list = take(room ? (size_t)(p.piece + 127) / 128 * 128 * a.top * 4 : 0);
     p.xt = take(a.dw ? (size_t)a.d * p.piece * es : 0);
     p.part = take(a.part_cap ? a.part_cap : std::max(dx_part, p.dw_splits > 1 ? (size_t)p.dw_splits * dw_rows * a.d * 4 : 0));
     p.dwa = take(a.dw && !a.dw_f32 && p.piece < a.n ? (size_t)dw_rows * a.d * 4 : 0);
@@ -410,7 +418,7 @@ __global__ __launch_bounds__(BS) void head_row_kernel(float* z_, int grads, Head
 struct HeadRef {
   const bf16_t *x, *w;
   bf16_t *xc, *dx;
-  int ldx, ldw, lddx, d, dp, n, np, V, top, vec;          // vec: rows of x are whole aligned groups of 8
+  int ldx, ldw, lddx, d, dp, n, np, V, top, vec, group;          // vec: rows of x are whole aligned groups of 8; group: entries per blockIdx.y, 1: the first one only
   const int32_t *pos, *count, *targets, *ids;
   const float* logits;
   const unsigned char* flags;
@@ -437,9 +445,17 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   bf16_t* xc = h.xc + (size_t)i * h.dp;
   float* zs = h.zsel + (size_t)i * (h.top + 1);
   float best = -INFINITY;
-  // Entries in groups of kRefGroup over blockIdx.y, the target (entry `top`) and the row's copy with the first; the reference is the largest of that first group.
+  // Entries in groups over blockIdx.y (the first entry alone, group 1, where the first product picks all logits), the target (entry `top`) and the row's copy with the first; the reference is the largest of that first group.
   constexpr int NB = 8;          // entries at a time: eight rows of W in flight
-  const int lo = blockIdx.y * kRefGroup, hi = soft ? min(lo + kRefGroup, h.top) : lo;
+  int lo = blockIdx.y * h.group, hi = soft ? min(lo + h.group, h.top) : lo;
+  if (h.group == 1 && soft) {          // the first entry there is
+    uint64_t there = 0;
+    for (int j = 0; j < h.top && !there; j += 64) {
+      const bool is = j + lane < h.top && (uint32_t)h.ids[(size_t)t * h.top + j + lane] < (uint32_t)h.V && h.logits[(size_t)t * h.top + j + lane] != -INFINITY;
+      there = __ballot(is);
+      if (there) { lo = j + __ffsll((unsigned long long)there) - 1; hi = lo + 1; }
+    }
+  }
   if (blockIdx.y && lo >= hi) return;
   const int list = hi - lo + (blockIdx.y == 0);          // entries of this wave, the target last
   for (int k0 = 0; k0 < list; k0 += NB) {
@@ -484,6 +500,53 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
       }
   }
   if (lane == 0 && blockIdx.y == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
+}
+
+// The entries of 128 compact rows sorted by groups of 64 columns, for the first product to pick their logits from its accumulators (HeadEpi's offs and list).  The order within a group
+// does not matter: every entry has a place of its own for its logit.  A block per 128 rows; dynamic shared memory: `groups` counters.
+__global__ __launch_bounds__(1024) void head_lists_kernel(const int32_t* __restrict__ rows, const int32_t* __restrict__ count, const int32_t* __restrict__ ids, const float* __restrict__ logits,
+                                                          const unsigned char* __restrict__ flags, int V, int top, int i0, int piece, int groups, int32_t* __restrict__ offs, int32_t* __restrict__ list) {
+  extern __shared__ int cnt[];
+  __shared__ int wave_sum_s[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, live = min(max(*count - i0, 0), piece), r0 = blockIdx.x * 128;
+  for (int g = tid; g < groups; g += 1024) cnt[g] = 0;
+  __syncthreads();
+  auto each = [&](auto f) {          // f(row in the 128, entry, id)
+    for (int x = tid; x < 128 * top; x += 1024) {
+      const int r = x / top, j = x - r * top;
+      if (r0 + r >= live) break;
+      const int t = rows[i0 + r0 + r];
+      if (!(flags[t] & ROW_SOFT)) continue;
+      const int id = ids[(size_t)t * top + j];
+      if ((uint32_t)id < (uint32_t)V && logits[(size_t)t * top + j] != -INFINITY) f(r, j, id);
+    }
+  };
+  each([&](int, int, int id) { atomicAdd(&cnt[id >> 6], 1); });
+  __syncthreads();
+  // counters to starts, 1024 groups at a time
+  int32_t* o = offs + (size_t)blockIdx.x * (groups + 1);
+  int base = 0;
+  for (int g0 = 0; g0 < groups; g0 += 1024) {
+    const int g = g0 + tid, mine = g < groups ? cnt[g] : 0;
+    int incl = mine;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+      const int v = __shfl_up(incl, k, 64);
+      if (lane >= k) incl += v;
+    }
+    __syncthreads();
+    if (lane == 63) wave_sum_s[wave] = incl;
+    __syncthreads();
+    int before = base, all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) { const int v = wave_sum_s[w]; if (w < wave) before += v; all += v; }
+    if (g < groups) { o[g] = before + incl - mine; cnt[g] = before + incl - mine; }
+    base += all;
+  }
+  if (tid == 0) o[groups] = base;
+  __syncthreads();
+  int32_t* l = list + (size_t)blockIdx.x * 128 * top;
+  each([&](int r, int j, int id) { l[atomicAdd(&cnt[id >> 6], 1)] = r | (id & 63) << 7 | j << 13; });
 }
 
 // A block per 16 compact rows of the piece: sums over the column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
@@ -1160,8 +1223,9 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
   bf16_t* e = p.grads ? (bf16_t*)(ws + p.z) : nullptr;
   const bf16_t* xc = (const bf16_t*)(ws + p.xc);
   bool ok = true;
-  head_ref_kernel<<<dim3((p.np + 3) / 4, std::max(1, (a.top + kRefGroup - 1) / kRefGroup)), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
-                                                       a.ldx % 8 == 0 && ((uintptr_t)a.x & 15) == 0, (const int32_t*)(ws + p.pos), count, a.targets, a.ids, a.logits, flags, zsel, ref, row_loss, a.row_lse});
+  const int group = p.pick ? 1 : kRefGroup;
+  head_ref_kernel<<<dim3((p.np + 3) / 4, p.pick ? 1 : std::max(1, (a.top + kRefGroup - 1) / kRefGroup)), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
+                                                       a.ldx % 8 == 0 && ((uintptr_t)a.x & 15) == 0, group, (const int32_t*)(ws + p.pos), count, a.targets, a.ids, a.logits, flags, zsel, ref, row_loss, a.row_lse});
   const float log2e = 1.44269504f;
   for (int i0 = 0; i0 < a.n; i0 += p.piece) {
     const int m = std::min(p.piece, p.np - i0);          // a multiple of 64
@@ -1169,11 +1233,16 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     auto* redo = (int32_t*)(ws + p.redo) + (size_t)(i0 / p.piece) * (1 + (p.piece + 255) / 256);
     HeadEpi he{};
     he.count = count; he.i0 = i0; he.piece = m; he.ref = ref; he.stats = stats; he.stats2 = stats2; he.k = p.mixed ? log2e : log2e / a.tau; he.kt = p.mixed ? log2e / a.tau : 0.f; he.vp = p.vp; he.tile = p.exp_tile;
+    if (p.pick) {
+      const int groups64 = (a.vocab + 255) / 256 * 4;
+      head_lists_kernel<<<(m + 127) / 128, 1024, groups64 * 4, st>>>(rows, count, a.ids, a.logits, flags, a.vocab, a.top, i0, m, groups64, (int32_t*)(ws + p.offs), (int32_t*)(ws + p.list));
+      he.offs = (const int32_t*)(ws + p.offs); he.list = (const int32_t*)(ws + p.list); he.zsel = zsel; he.top = a.top;
+    }
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
               !p.mixed, redo, a.tau, a.share};
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
-    he.redo = redo;
+    he.redo = redo; he.offs = nullptr;          // the logits are picked already
     f.again = 1;
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);

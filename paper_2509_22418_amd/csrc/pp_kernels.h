@@ -19,7 +19,7 @@ struct ShadowSeg {      // one trainable row block that also lives, transposed, 
 };
 
 enum { EPI_STORE = 0, EPI_ADD_RES = 1, EPI_SWIGLU = 2, EPI_SWIGLU_BWD = 3, EPI_ROPE = 4,          // the last three: only inside k_gemm_swiglu_*_mfma / k_gemm_qkv_rope_mfma
-       EPI_HEAD_EXP = 5, EPI_HEAD_DX = 6, EPI_HEAD_PART = 7, EPI_HEAD_DW = 8, EPI_HEAD_DW_PART = 9 };          // only inside k_head_gemm
+       EPI_HEAD_EXP = 5, EPI_HEAD_DX = 6, EPI_HEAD_PART = 7, EPI_HEAD_DW = 8, EPI_HEAD_DW_PART = 9, EPI_HEAD_EXP_PICK = 10 };          // only inside k_head_gemm
 
 void k_fill_f32(hipStream_t st, float* p, size_t n, float v);
 void k_rope_tables(hipStream_t st, float* cosb, float* sinb, int S, int dh, float base);
@@ -152,6 +152,11 @@ struct HeadEpi {
   float k, kt;
   int tile;                        // 0: 256 x 256 tiles, groups of 64 columns; 128, 64: the smaller-tile GEMM's, groups of 32
   int vp;
+  // Entries whose logits are wanted (nullptr: none): those of rows 128 h .. and columns 64 g .. are list[128 h top + offs[h][g]] up to offs[h][g + 1] (pitch of offs: groups of 64 columns of the
+  // tiles, plus one), each row in the 128 (7 bits), column in the 64 (6 bits), place j among the row's entries: z goes to zsel[row of all][j], rows of top + 1
+  const int32_t *offs, *list;
+  float* zsel;
+  int top;
   const int32_t* redo;             // nullptr, or: [0] != 0 if any, [1 + b] != 0 if rows 256 b .. are to be done (nothing else is)
   // the others: columns of B that can be read, a multiple of 8
   int ncols;

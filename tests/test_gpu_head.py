@@ -98,10 +98,9 @@ def check(got, x, w, y, ids=None, u=None, tau=1.0, share=1.0, weight=None, dw=No
                 off[t, Y[t]] += abs(g[t]) * (1 - share)
     if ids is not None:
         I = ints(ids)
-        for t in np.nonzero(live)[0]:
-            for i in I[t]:
-                if 0 <= i < vocab:
-                    off[t, i] = abs(g[t]) * (1 + share * tau)
+        rows = np.broadcast_to(np.arange(n)[:, None], I.shape)
+        there = (I >= 0) & (I < vocab) & live[:, None]
+        off[rows[there], I[there]] = np.abs(g[rows[there]]) * (1 + share * tau)
     # with both softmaxes at different temperatures one is a power of the other's rounded value
     both = 1.0 if tau == 1.0 or share in (0.0, 1.0) else 1.0 + it
     err = part * (ez_rel * both) + off * (4 * rel[:, None] + 16 * EPS)
@@ -178,6 +177,22 @@ def test_pieces_strides_slices_and_weights(kind, dtype):
         f = call(x, w, y, weight=weight, dw=(lo, hi), piece=piece, pad=2, dw_type=torch.float32, **a)
         check(f, x, w, y, weight=weight, dw=(lo, hi), **a)
         check(call(x, w, y, weight=weight, dx=False, dw=(lo, hi), piece=piece, dw_type=torch.float32, dw_add=True, pad=1, **a), x, w, y, weight=weight, dw=(lo, hi), base=7.0, pieces=-(-n // piece) if piece else 1, **a)
+
+
+@pytest.mark.parametrize("n,vocab,d,top,piece", [(3000, 5000, 256, 128, 0), (2801, 6001, 200, 120, 0), (5000, 3001, 128, 128, 2944)])
+@pytest.mark.parametrize("tau,share", [(1.0, 0.5), (2.0, 1.0), (2.0, 0.6)])
+def test_entries_picked_from_the_product(n, vocab, d, top, piece, tau, share):
+    """Enough entries for their logits to be picked from the first product: lists of all lengths (none for whole blocks of rows), a quarter of all entries on one column, equal ids within
+    rows, the last tiles ragged."""
+    print(f"case head picked {n}x{vocab}x{d} top={top} tau={tau} share={share} piece={piece}", flush=True)
+    x, w, y, ids, u = make(n, vocab, d, torch.bfloat16, top=top, seed=13)
+    there = (ids >= 0) & (ids < vocab)          # absent entries hold NaN and stay absent
+    ids[::4] = torch.where(there[::4], vocab - 1, ids[::4].long()).int()
+    ids[7] = torch.where(there[7], 5, ids[7].long()).int()
+    ids[512:768] = -1
+    y[600:700] = -1
+    a = dict(ids=ids, u=u, tau=tau, share=share)
+    check(call(x, w, y, dw=(0, vocab), piece=piece, **a), x, w, y, dw=(0, vocab), **a)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
