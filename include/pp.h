@@ -59,7 +59,7 @@ typedef struct {
                                  bit for bit; WORKSPACE shrinks by about (n_layers - 1) layers of activations.
                                  PP_HEAD_PIECES may be added to either (a bit): the output head's logits are not kept either.  Its loss and gradients
                                  are formed a piece of rows at a time (pp_op_head_ce in pp_ops.h states how, and the roundings; with bf16 storage the loss is
-                                 formed from fp32 logits, not from rounded ones), WORKSPACE holds at most about 1.5 GiB for them instead of B x S x vocab elements, and
+                                 formed from fp32 logits, not from rounded ones), WORKSPACE holds about 0.4 GB and one copy of the final norm's output for them instead of B x S x vocab elements, and
                                  vocab may be up to 2^20 (without: 65536 with bf16 storage, 16320 with fp32). */
 } pp_config;
 enum { PP_HEAD_PIECES = 4 };

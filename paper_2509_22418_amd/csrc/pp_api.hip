@@ -104,6 +104,7 @@ static HeadArgs step_head(const pp_config& c, bool dw, bool dx, int n) {
   a.dtype = c.dtype; a.n = n; a.vocab = c.vocab; a.ldwt = c.vocab;
   a.dw_hi = dw ? c.vocab : 0; a.dw_f32 = 1;
   a.tau = 1.f;
+  a.piece = std::max(256, (int)((256ull << 20) / ((size_t)c.vocab * esize(c)) / 256 * 256));          // a quarter of the logits of 16384 x 32000 in bf16
   a.part_cap = kPartialCap;
   a.no_few = 1;
   return a;

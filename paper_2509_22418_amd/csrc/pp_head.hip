@@ -193,68 +193,55 @@ __global__ __launch_bounds__(256) void head_flags_kernel(const int32_t* __restri
   if (lane == 0) flags[t] = weight && weight[t] == 0.f ? 0 : (hard_row(targets, t, V) ? ROW_HARD : 0) | (soft ? ROW_SOFT : 0);
 }
 
-// pos[t] = place of row t among the rows that count, -1 for the others; rows[i] = t; count = their number; redo cleared.  One block; 16 consecutive rows per thread.
+// pos[t] = place of row t among the rows that count, -1 for the others; rows[i] = t; count = their number; redo cleared.  One block, 16 rows per thread at a time: rows 1024 apart, so that
+// what a wave reads and writes lies together.
 __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restrict__ targets, const unsigned char* __restrict__ flags, const float* __restrict__ weight, int n, int V,
                                                          int32_t* __restrict__ pos, int32_t* __restrict__ rows, int32_t* __restrict__ count, int32_t* __restrict__ redo, int n_redo, int pieces, int piece,
                                                          int tiles_d, int steps, int most, size_t cap, int d) {
-  __shared__ int wave_sum_s[16];
+  __shared__ int total_s, part_s[256];          // rows that count of wave w in the e-th 1024 at [16 e + w]; then those before them
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < n_redo; i += 1024) redo[i] = 0;
-  const bool vec = ((uintptr_t)targets & 15) == 0 && ((uintptr_t)weight & 15) == 0;
   int base = 0;
   for (int t0 = 0; t0 < n; t0 += 16 * 1024) {
-    const int first = t0 + tid * 16;
     uint32_t live = 0;
-    if (flags) {          // flags and pos are 256-byte aligned and padded to 64 rows
-      if (first < n) {
-        const uint4 f = *reinterpret_cast<const uint4*>(flags + first);
-        const uint32_t w[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) live |= ((w[e >> 2] >> (8 * (e & 3)) & 255) != 0 && first + e < n ? 1u : 0u) << e;
-      }
-    } else if (vec && first + 16 <= n) {
-      int4 y[4];
-      float4 g[4];
+    for (int e = 0; e < 16; ++e) {
+      const int t = t0 + e * 1024 + tid;
+      if (t < n && (flags ? flags[t] != 0 : hard_row(targets, t, V) && !(weight && weight[t] == 0.f))) live |= 1u << e;
+    }
+    uint64_t ballot[16];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        y[q] = *reinterpret_cast<const int4*>(targets + first + 4 * q);
-        g[q] = weight ? *reinterpret_cast<const float4*>(weight + first + 4 * q) : make_float4(1.f, 1.f, 1.f, 1.f);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        auto one = [&](int v, float gv) { return (uint32_t)v < (uint32_t)V && gv != 0.f ? 1u : 0u; };
-        live |= (one(y[q].x, g[q].x) | one(y[q].y, g[q].y) << 1 | one(y[q].z, g[q].z) << 2 | one(y[q].w, g[q].w) << 3) << (4 * q);
-      }
-    } else
-      for (int e = 0; e < 16 && first + e < n; ++e)
-        if (hard_row(targets, first + e, V) && !(weight && weight[first + e] == 0.f)) live |= 1u << e;
-    const int mine = __popc(live);
-    int incl = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(incl, o, 64);
-      if (lane >= o) incl += v;
+    for (int e = 0; e < 16; ++e) {
+      ballot[e] = __ballot(live >> e & 1);
+      if (lane == 0) part_s[16 * e + wave] = __popcll(ballot[e]);
     }
     __syncthreads();
-    if (lane == 63) wave_sum_s[wave] = incl;
-    __syncthreads();
-    int before = base, all = 0;
+    if (wave == 0) {          // exclusive sums of the 256 parts, four per lane
+      int v[4], sum = 0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) { const int v = wave_sum_s[w]; if (w < wave) before += v; all += v; }
-    const int at0 = before + incl - mine;
-    if (first < n) {
-      int at = at0;
-      int pv[16];
+      for (int k = 0; k < 4; ++k) { v[k] = part_s[4 * lane + k]; sum += v[k]; }
+      int incl = sum;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const bool l = live >> e & 1;
-        pv[e] = l ? at : -1;
-        if (l) rows[at++] = first + e;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(incl, o, 64);
+        if (lane >= o) incl += u;
       }
+      int before = incl - sum;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) *reinterpret_cast<int4*>(pos + first + 4 * q) = make_int4(pv[4 * q], pv[4 * q + 1], pv[4 * q + 2], pv[4 * q + 3]);
+      for (int k = 0; k < 4; ++k) { part_s[4 * lane + k] = before; before += v[k]; }
+      if (lane == 63) total_s = before;
     }
-    base += all;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int t = t0 + e * 1024 + tid, at = base + part_s[16 * e + wave] + __popcll(ballot[e] & ((1ull << lane) - 1));
+      if (t >= n) continue;
+      const bool l = live >> e & 1;
+      pos[t] = l ? at : -1;
+      if (l) rows[at] = t;
+    }
+    base += total_s;
+    __syncthreads();
   }
   if (tid == 0) *count = base;
   for (int i = tid; i < pieces; i += 1024) {          // every piece's ranges of dX's contraction
