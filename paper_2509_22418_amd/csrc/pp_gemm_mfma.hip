@@ -529,26 +529,39 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         }
       }
     }
-    if (he.kt != 0.f) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float off2 = -rk[i] * he.kt;
-        float s2 = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) s2 += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], he.kt, off2));
-        s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64);
-        if (eq == 0 && row0 + 16 * i < M) he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = s2;
-      }
-    }
     // sum / maximum over the four lanes that hold a row's columns: row swaps in registers instead of trips through LDS
     auto swap16 = [](float v) { return __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
     auto swap32 = [](float v) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
+    if (he.kt != 0.f) {          // two softmaxes: both sums, and the exponents in place of the logits
+      const float km = fmaxf(he.k, he.kt);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float off = -rk[i] * he.k, off2 = -rk[i] * he.kt, offm = -rk[i] * km;
+        float s = 0.f, s2 = 0.f, t = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float z = acc[i][j][r], y = fmaf(z, he.k, off);
+            t = fmaxf(t, y);
+            s += __builtin_amdgcn_exp2f(y);
+            s2 += __builtin_amdgcn_exp2f(fmaf(z, he.kt, off2));
+            acc[i][j][r] = head_exponent_code(fmaf(z, km, offm));
+          }
+        s += __shfl_xor(s, 16, 64); s += __shfl_xor(s, 32, 64);
+        s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64);
+        t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
+        if (eq == 0 && row0 + 16 * i < M) {
+          he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
+          he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = s2;
+        }
+      }
+    }
     const bool keep = C && n0 + wn * 64 < he.vp;
     stores = !keep || m0 + BM <= M ? 8 : 0;          // vector memory instructions issued for certain behind everything else: the second half's stores, or the next tile's references
 #pragma unroll
     for (int hi = 0; hi < 2; ++hi) {          // half of the rows at a time: the first half's stores leave while the second's exponentials are formed
+      if (he.kt == 0.f)
 #pragma unroll
       for (int ii = 0; ii < 4; ++ii) {
         const int i = 4 * hi + ii;

@@ -12,7 +12,7 @@
 // a kernel over rows replaces e at those few places, and C is applied to dX's rows behind their product and to X's rows in front of dW's.  No other pass over the piece, and no second
 // product of logits: 2 products for dX alone, 3 with dW.  Rows whose largest logit turns out to lie more than kFar above the reference take the maximum, and the first product of
 // their 256-row blocks is done again (by a launch that ends at once where there are none).  Two softmaxes at once (tau != 1 beside hard targets) take one more pass
-// over the piece, which forms the second's exponentials as powers of the first's.
+// over the piece, which forms both exponentials from the one exponent that the first product then stores.
 // Pieces are of rows, not of the vocabulary: a piece of vocabulary would have to wait for the sums of all others, hence form its logits twice (4 products instead of 3), and sum dX in
 // memory.  fp32: logits in fp32, softmax and dz by a block per row, products on the fp32 MFMA kernels.
 #include "pp_kernels.h"
@@ -702,21 +702,22 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
   }
 }
 
-// Two softmaxes: e1 = exp(z - r) becomes (p1 e1 + pt e1^(1 / tau)) / C, in front of head_fin's places.  The power's argument lies within a row's rounded e1; its relative error is 1 / tau of it.
-__global__ __launch_bounds__(256) void head_mix_kernel(bf16_t* e, int vp, const float2* __restrict__ coef, const int32_t* __restrict__ count, int i0, int piece, float it) {
+// Two softmaxes: the stored exponents (head_exponent_code) become (p1 e1 + pt et) / C, in front of head_fin's places.  k1, kt: of the two softmaxes in units of the sharper one's exponent,
+// which is the one that is stored.
+__global__ __launch_bounds__(256) void head_mix_kernel(bf16_t* e, int vp, const float2* __restrict__ coef, const int32_t* __restrict__ count, int i0, int piece, float k1, float kt) {
   const int i = blockIdx.x;
   if (i >= min(max(*count - i0, 0), piece)) return;
   const float2 c = coef[i];
   uint4* row = reinterpret_cast<uint4*>(e + (size_t)i * vp);
+  auto mixed = [&](uint32_t code) {
+    const float y = head_exponent(code);
+    return c.x * __builtin_amdgcn_exp2f(y * k1) + c.y * __builtin_amdgcn_exp2f(y * kt);
+  };
   for (int v = threadIdx.x; v < vp / 8; v += 256) {
-    uint4 r = row[v];
+    const uint4 r = row[v];
     uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float a = __uint_as_float(w[k] << 16), b = __uint_as_float(w[k] & 0xffff0000u);
-      // e1 = 0 (lost, or behind the vocabulary): log2 = -inf, power 0
-      w[k] = f32x2_to_bf16x2(c.x * a + c.y * __builtin_amdgcn_exp2f(it * __builtin_amdgcn_logf(a)), c.x * b + c.y * __builtin_amdgcn_exp2f(it * __builtin_amdgcn_logf(b)));
-    }
+    for (int k = 0; k < 4; ++k) w[k] = f32x2_to_bf16x2(mixed(w[k] & 0xffff), mixed(w[k] >> 16));
     row[v] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
@@ -1235,7 +1236,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     if (!e) continue;
     if (p.mixed) {
-      head_mix_kernel<<<m, 256, 0, st>>>(e, p.vp, coef, count, i0, m, 1.0f / a.tau);
+      head_mix_kernel<<<m, 256, 0, st>>>(e, p.vp, coef, count, i0, m, std::min(1.f, a.tau), std::min(1.f, 1.f / a.tau));
       f.again = 0; f.places = 1;
       head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     }

@@ -145,7 +145,7 @@ struct HeadEpi {
   const int32_t* count;
   int i0, piece;
   // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and group of columns the sum of e, the largest exponent and, where kt != 0,
-  // the sum of exp2(kt (z - ref)), at [group][row of the piece].
+  // the sum of exp2(kt (z - ref)), at [group][row of the piece].  Where kt != 0, C holds not e but the exponent max(k, kt) (z - ref) as head_exponent_code makes it.
   const float* ref;
   float2* stats;
   float* stats2;
@@ -170,6 +170,18 @@ struct HeadEpi {
   int ldadd, out_f32;
   int vec;                         // DX, DW: rows of C (and add) are whole aligned groups of 8
 };
+// An exponent y <= 60 in 16 bits, for two softmaxes: each may need what the other's exponential has lost (exp(-100) is nothing in bf16, exp(-100 / 64) is not).  Steps of 2^-8 from -64 on
+// (exp2's relative error at most 2^-9 ln 2, less than the half step of a bf16 exponential), which is where the sharper softmax has its weight; below, down to -2096, steps of 2^-4: the
+// sharper exponential is below 2^-64 there, and the softer's error is 2^-5 ln 2 over the ratio of the temperatures, on a weight of at most 2^(-64 / ratio).  The code is the upper half
+// of a normal float, so that rounding that float to bf16 stores it: 0x0080 + step, 0x8080 + step below -64, 0xff7f for nothing at all.
+__device__ __forceinline__ float head_exponent_code(float y) {
+  const float w = y + 64.f, steps = fminf(fmaxf(256.f * w, -16.f * w) + 128.5f, 0x7f7f);          // without a choice: the epilogues that call this have no registers for its masks
+  return __uint_as_float((uint32_t)steps << 16 | (__float_as_uint(w) & 0x80000000u));
+}
+__device__ __forceinline__ float head_exponent(uint32_t code) {
+  if (code == 0xff7f) return -INFINITY;
+  return code & 0x8000 ? (float)(0x8080 - 64 * 16 - (int)code) * 0.0625f : (float)((int)code - 0x0080) * (1.f / 256) - 64.f;
+}
 // The exponentials on the smaller-tile GEMM's tiles (he.tile); head_exp_ring: which pay for M rows at most, 0: none
 int head_exp_ring(int M, int N, int K);
 int k_head_exp_ring(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he);

@@ -254,6 +254,17 @@ def far(n, kind, dtype):
     check(call(x, w, y, dx=False, **a), x, w, y, **a)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,vocab", [(40, 600), (2100, 4100)])
+@pytest.mark.parametrize("tau,std", [(64.0, 30.0), (16.0, 30.0), (3.0, 8.0), (0.125, 8.0), (1.0 / 64, 1.0)])
+def test_two_softmaxes_of_logits_far_apart(tau, std, n, vocab, dtype):
+    """Hard targets and a teacher at a temperature far from 1: where one softmax has nothing left of a logit (hundreds below the largest), the other still has."""
+    x, w, y, ids, u = make(n, vocab, 64, TYPES[dtype], top=6, std=std, seed=4)
+    a = dict(ids=ids, u=u, tau=tau, share=0.6)
+    dw = (3, vocab // 2)
+    check(call(x, w, y, dw=dw, **a), x, w, y, dw=dw, **a)
+
+
 def test_non_finite_rows_that_count_stay_in_their_rows():
     """NaN in a row that counts: its loss and its dX row are NaN, the other rows' are as without it."""
     x, w, y, _, _ = make(300, 500, 64, torch.bfloat16, ignored=0.0)
