@@ -77,8 +77,9 @@ int pp_op_attention_bwd(void* hip_stream, int dtype, const void* qkv_dev, const 
  *                       either (terms with a share of 0 do not count) is left out.
  * A row of weight 0 is left out too.  Rows that are left out have row_loss = row_lse = 0 and a dX row of zeros, and neither their values nor infinities or NaN among them reach
  * anything else.  n == 0 gives loss 0 and dW = 0.
- * Sums, exponentials and losses are fp32.  With bf16 storage the exponentials of a row are rounded to bf16 (at most 2^-8 relative) on their way into the gradients'
- * products, as are the rows of X scaled by w_t over the softmax's sum; dX is rounded once from fp32 sums.  Results do not depend on the run. */
+ * Sums, exponentials and losses are fp32.  With bf16 storage and more than 16 rows, a row of dz enters the gradients' products as a multiple of a row that is rounded to
+ * bf16 (at most 2^-8 relative, twice where both softmaxes count at a temperature other than 1), its multiple moved by at most 2^-8 so that the largest element is not rounded; the rows of X are
+ * scaled by the multiple and rounded to bf16 for dW.  dX and dW are rounded once from fp32 sums.  Results do not depend on the run. */
 #define PP_HEAD_TOP_MAX 128
 typedef struct {
   const void *x, *w;               /* storage type dtype */
@@ -90,7 +91,8 @@ typedef struct {
   int32_t dtype, n, vocab, d;      /* PP_F32 or PP_BF16; n <= 2^24, vocab <= 2^20, d <= 2^14 */
   int32_t dw_lo, dw_hi;            /* 0 <= dw_lo <= dw_hi <= vocab; row 0 of dw is row dw_lo of W */
   int32_t dw_f32;                  /* 0: dw in storage type; 1: dw float; 2: dw float, and the gradient is added to what it holds */
-  int32_t piece;                   /* rows of a piece, rounded up to a multiple of 64; 0: as many as keep a piece's buffer within 512 MiB */
+  int32_t piece;                   /* rows of a piece, rounded up to a multiple of 64 and at most as many as keep a piece's buffer within 2 GiB (256 rows in any case);
+                                      0: as many as keep it within 512 MiB, or within the size of dW's float sums, up to 1 GiB, where that is larger */
 } pp_head;
 /* Workspace of a call with these sizes, options and operand alignment (top: entries per row, 0 for pp_op_head_ce); 0 and an error text on invalid arguments. */
 size_t pp_op_head_bytes(const pp_head* head, int32_t top);

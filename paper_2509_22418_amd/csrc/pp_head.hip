@@ -102,7 +102,8 @@ HeadPlan plan_head(const HeadArgs& a) {
   // Every piece but the first reads and writes dW's fp32 sums: with a larger dW the pieces may be as large as that, up to 1 GiB (4096 x 4096 x 128000, in two pieces / in one: 10.5 / 9.5 ms)
   const size_t limit = std::max(kPieceBytes, std::min(2 * kPieceBytes, (size_t)dw_rows * a.d * 4));
   p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(limit / row / 256 * 256));
-  p.piece = std::min(std::min(p.piece, p.np), 1 << 18);          // grids of piece / 64 in y
+  // 2^18: grids of piece / 64 in y.  2 GiB: the products' 32-bit offsets and whatever a caller asks for
+  p.piece = std::min({p.piece, p.np, 1 << 18, std::max(256, (int)((2ull << 30) / row / 256 * 256))});
   // columns that one partial sum of a row covers, by the tiles of the first product; the last piece, which may be smaller, takes the tiles of the others
   p.exp_tile = bf ? head_exp_ring(p.piece, a.vocab, p.dp) : 0;
   const int wide = p.exp_tile ? p.exp_tile : 256;
@@ -112,8 +113,8 @@ HeadPlan plan_head(const HeadArgs& a) {
   const double rounds = (double)((p.piece + 255) / 256) * ((a.vocab + 255) / 256) / 256;
   p.pick = bf && a.top && !p.exp_tile && a.vocab <= 1 << 19 &&          // (the lists' counters fit 32 KB of LDS)
            (double)p.piece * a.top * p.dp * 2 / 7e6 > 15 + 1.2 * rounds;
-  // the bf16 matrix kernels read rows that are multiples of 64 elements long and 16-byte aligned, the fp32 ones any
-  p.copy_w = bf && (a.d % 64 || a.ldw % 8 || (uintptr_t)a.w & 15);
+  // the bf16 matrix kernels read rows that are multiples of 64 elements long, 16-byte aligned and not so far apart that the offsets among 64 of them pass 31 bits; the fp32 ones any
+  p.copy_w = bf && (a.d % 64 || a.ldw % 8 || a.ldw > 1 << 22 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
   // dX's ranges are decided on the device by the rows that count (head_scan_kernel): at most so many, and partial sums for the worst number of rows
   const int tiles_d = (a.d + 255) / 256;

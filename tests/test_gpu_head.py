@@ -265,6 +265,18 @@ def test_two_softmaxes_of_logits_far_apart(tau, std, n, vocab, dtype):
     check(call(x, w, y, dw=dw, **a), x, w, y, dw=dw, **a)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [5, 40])
+def test_rows_far_apart_in_memory(n, dtype):
+    """Rows of W and X so long that the offsets of 64 of them pass 31 bits."""
+    ld, d, vocab = (1 << 24) + 8, 64, 70
+    x, w, y, _, _ = make(n, vocab, d, TYPES[dtype])
+    far_w, far_x = torch.empty((vocab, ld), dtype=w.dtype, device="cuda")[:, :d], torch.empty((n, ld), dtype=x.dtype, device="cuda")[:, :d]
+    far_w.copy_(w)
+    far_x.copy_(x)
+    check(call(far_x, far_w, y, dw=(1, 69)), x, w, y, dw=(1, 69))
+
+
 def test_non_finite_rows_that_count_stay_in_their_rows():
     """NaN in a row that counts: its loss and its dX row are NaN, the other rows' are as without it."""
     x, w, y, _, _ = make(300, 500, 64, torch.bfloat16, ignored=0.0)

@@ -177,3 +177,10 @@ def test_model_without_kept_logits_plans_less_and_takes_larger_vocabularies():
     for bad in (2, 3, 6, 8, -1):
         c = b.make_config(dict(cfg, recompute=bad))
         assert lib.pp_query_bytes(ctypes.byref(c), None, 0) == 0 and "recompute" in b.pp_last_error()
+
+
+def test_workspace_is_bounded_for_any_piece():
+    """A piece asked for in rows is cut to 2 GiB of logits; smaller ones are as large as asked."""
+    size = lambda piece: pp.pp_op_head_bytes(head(n=1 << 18, vocab=1 << 20, d=64, ldx=64, ldw=64, lddx=64, dw_lo=0, dw_hi=0, dw=None, piece=piece), 0)  # noqa: E731
+    assert size(1 << 24) == size(1024) > size(960)
+    assert size(1 << 24) <= (2 << 30) + (1 << 30)
