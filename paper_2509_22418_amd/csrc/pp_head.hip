@@ -44,13 +44,13 @@ int pad_to(long v, int m) { return (int)((v + m - 1) / m * m); }
 // partial sums to write), and the launch that sums them 5 us and 0.1 us per tile and range.  (32000 x 768 over 8192 rows, 375 tiles: one range 415 us, two 397 + 73; 8192 x 768 over 32000,
 // 96 tiles: two 412 + 14, five 402 + 28; 3277 x 2048 over 32000, 104 tiles: one 572, two 345 + 26.)
 constexpr int kMaxSplits = 32;
-__host__ __device__ inline int best_splits(int tiles, int steps, int most) {
-  int best = 1, cost = 0;
-  if (tiles > 1024) return 1;
-  for (int s = 1; s <= most && steps >= 8 * s; ++s) {
-    const int c = (tiles * s + 255) / 256 * ((steps + s - 1) / s * 32 / 5 + (s > 1 ? 120 : 40)) + (s > 1 ? 20 + s * tiles * 2 / 5 : 0);
-    if (s == 1 || c < cost) { best = s; cost = c; }
-  }
+__host__ __device__ inline int splits_cost(int tiles, int steps, int s) {
+  return (tiles * s + 255) / 256 * ((steps + s - 1) / s * 32 / 5 + (s > 1 ? 120 : 40)) + (s > 1 ? 20 + s * tiles * 2 / 5 : 0);
+}
+int best_splits(int tiles, int steps, int most) {
+  int best = 1;
+  for (int s = 2; s <= most && steps >= 8 * s && tiles <= 1024; ++s)
+    if (splits_cost(tiles, steps, s) < splits_cost(tiles, steps, best)) best = s;
   return best;
 }
 // ranges that fit the buffer of the partial sums
@@ -205,11 +205,20 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
   int base = 0;
   for (int t0 = 0; t0 < n; t0 += 16 * 1024) {
     uint32_t live = 0;
+    int32_t y[16];          // all of a thread's loads in flight, from clamped places
+    float g[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const int t = t0 + e * 1024 + tid;
-      if (t < n && (flags ? flags[t] != 0 : hard_row(targets, t, V) && !(weight && weight[t] == 0.f))) live |= 1u << e;
+      y[e] = -1;
+      g[e] = 1.f;
+      if (t0 + e * 1024 >= n) continue;
+      const int t = min(t0 + e * 1024 + tid, n - 1);
+      y[e] = flags ? flags[t] : targets[t];
+      if (weight && !flags) g[e] = weight[t];
     }
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (t0 + e * 1024 + tid < n && (flags ? y[e] != 0 : (uint32_t)y[e] < (uint32_t)V && g[e] != 0.f)) live |= 1u << e;
     uint64_t ballot[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -245,11 +254,17 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
     __syncthreads();
   }
   if (tid == 0) *count = base;
-  for (int i = tid; i < pieces; i += 1024) {          // every piece's ranges of dX's contraction
-    const int live = min(max(base - i * piece, 0), piece), rows = (live + 63) & ~63;
-    int s = best_splits((live + 255) / 256 * tiles_d, steps, most);
+  for (int i = wave; i < pieces; i += 16) {          // every piece's ranges of dX's contraction (best_splits), a number of ranges per lane
+    const int live = min(max(base - i * piece, 0), piece), rows = (live + 63) & ~63, mine = lane + 1;
+    static_assert(kMaxSplits <= 64, "a lane each");
+    const int cost = splits_cost((live + 255) / 256 * tiles_d, steps, mine);
+    const bool can = mine == 1 || (mine <= most && steps >= 8 * mine && (live + 255) / 256 * tiles_d <= 1024);
+    int low = can ? cost : 0x7fffffff;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) low = min(low, __shfl_xor(low, o, 64));
+    int s = __ffsll((unsigned long long)__ballot(can && cost == low));
     while (s > 1 && cap && (double)s * rows * d * 4 > (double)cap) --s;
-    redo[n_redo + i] = s;
+    if (lane == 0) redo[n_redo + i] = s;
   }
 }
 
@@ -704,22 +719,25 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
 }
 
 // Two softmaxes: the stored exponents (head_exponent_code) become (p1 e1 + pt et) / C, in front of head_fin's places.  k1, kt: of the two softmaxes in units of the sharper one's exponent,
-// which is the one that is stored.
+// which is the one that is stored.  A block per row and 8192 columns.
 __global__ __launch_bounds__(256) void head_mix_kernel(bf16_t* e, int vp, const float2* __restrict__ coef, const int32_t* __restrict__ count, int i0, int piece, float k1, float kt) {
-  const int i = blockIdx.x;
+  const int i = blockIdx.x, v0 = blockIdx.y * 1024 + threadIdx.x;
   if (i >= min(max(*count - i0, 0), piece)) return;
   const float2 c = coef[i];
   uint4* row = reinterpret_cast<uint4*>(e + (size_t)i * vp);
+  uint4 r[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) r[m] = row[min(v0 + 256 * m, vp / 8 - 1)];
   auto mixed = [&](uint32_t code) {
     const float y = head_exponent(code);
     return c.x * __builtin_amdgcn_exp2f(y * k1) + c.y * __builtin_amdgcn_exp2f(y * kt);
   };
-  for (int v = threadIdx.x; v < vp / 8; v += 256) {
-    const uint4 r = row[v];
-    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    uint32_t w[4] = {r[m].x, r[m].y, r[m].z, r[m].w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) w[k] = f32x2_to_bf16x2(mixed(w[k] & 0xffff), mixed(w[k] >> 16));
-    row[v] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (v0 + 256 * m < vp / 8) row[v0 + 256 * m] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -1237,7 +1255,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     if (!e) continue;
     if (p.mixed) {
-      head_mix_kernel<<<m, 256, 0, st>>>(e, p.vp, coef, count, i0, m, std::min(1.f, a.tau), std::min(1.f, 1.f / a.tau));
+      head_mix_kernel<<<dim3(m, (p.vp / 8 + 1023) / 1024), 256, 0, st>>>(e, p.vp, coef, count, i0, m, std::min(1.f, a.tau), std::min(1.f, 1.f / a.tau));
       f.again = 0; f.places = 1;
       head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
     }
