@@ -108,11 +108,12 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.exp_tile = bf ? head_exp_ring(p.piece, a.vocab, p.dp) : 0;
   const int wide = p.exp_tile ? p.exp_tile : 256;
   p.groups = (a.vocab + wide - 1) / wide * (wide / (p.exp_tile ? 32 : 64));
-  // Logits of the teacher's entries: by dot products (head_ref_kernel), a row of W each (7 TB/s, out of the last-level cache), or picked from the first product's accumulators (12 us for the lists and
-  // about 1.2 us for each round of tiles: 8192 x 2048 x 32000 with 64 entries a row 315 us / 50 us).
+  // Logits of the teacher's entries: by dot products (head_ref_kernel: a row of W each, 7 TB/s out of the last-level cache, half a microsecond for each of a wave's up to 16), or picked from the first
+  // product's accumulators (the lists, and their look-ups in every tile; 8192 x 2048 x 32000 with 64 entries a row 315 us / 50 us).  In us, fitted to 165 shapes timed both ways (widths of 256 to 2048, 700
+  // to 8000 rows, vocabularies of 8000 to 100000, 2 to 64 entries): on 159 the rule takes the faster or one within 3 % of it, on the others one within 7 %.
   const double rounds = (double)((p.piece + 255) / 256) * ((a.vocab + 255) / 256) / 256;
   p.pick = bf && a.top && !p.exp_tile && a.vocab <= 1 << 19 &&          // (the lists' counters fit 32 KB of LDS)
-           (double)p.piece * a.top * p.dp * 2 / 7e6 > 15 + 1.2 * rounds;
+           (double)p.piece * a.top * p.dp * 2 / 7e6 + std::min(a.top, 16) / 2. > 6 + a.top / 12. + rounds * a.vocab / 9e4;
   // the bf16 matrix kernels read rows that are multiples of 64 elements long, 16-byte aligned and not so far apart that the offsets among 64 of them pass 31 bits; the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || a.ldw > 1 << 22 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
