@@ -1141,6 +1141,7 @@ static int check_head(const pp_head* h, int top, HeadArgs* a) {
 static int run_head(const char* who, void* hip_stream, const HeadArgs& a, void* ws, size_t ws_bytes) {
   if (!ws || ((uintptr_t)ws & 255)) return fail(PP_EINVAL, std::string(who) + ": workspace is NULL or not 256-byte aligned");
   if (ws_bytes < head_bytes(a)) return fail(PP_EINVAL, std::string(who) + ": workspace of " + std::to_string(ws_bytes) + " bytes, needs " + std::to_string(head_bytes(a)) + " (pp_op_head_bytes)");
+  if ((a.dx && (a.dx == a.x || a.dx == a.w)) || (a.dw && (a.dw == a.x || a.dw == a.w || a.dw == a.dx))) return fail(PP_EINVAL, std::string(who) + ": dx or dw is in the place of another operand");
   int dev = 0;
   hipDevice_t own = 0;
   if (hip_stream) {

@@ -184,3 +184,11 @@ def test_workspace_is_bounded_for_any_piece():
     size = lambda piece: pp.pp_op_head_bytes(head(n=1 << 18, vocab=1 << 20, d=64, ldx=64, ldw=64, lddx=64, dw_lo=0, dw_hi=0, dw=None, piece=piece), 0)  # noqa: E731
     assert size(1 << 24) == size(1024) > size(960)
     assert size(1 << 24) <= (2 << 30) + (1 << 30)
+
+
+@pytest.mark.parametrize("over", [dict(dx=0x1000), dict(dx=0x2000), dict(dw=0x1000), dict(dw=0x2000), dict(dw=0x3000)])
+def test_gradients_in_the_place_of_operands_are_refused(over):
+    h = head(**dict(dict(x=0x1000, w=0x2000, dx=0x3000, dw=0x4000), **over))
+    for call in (lambda: pp.pp_op_head_ce(None, h, 0x1000, 0x1000, 1 << 40), lambda: pp.pp_op_head_distill(None, h, 0x1000, 0x1000, 4, 1.0, 0.5, 0x1000, 0x1000, 1 << 40)):
+        with pytest.raises(pp.PPError, match="place of another"):
+            call()
