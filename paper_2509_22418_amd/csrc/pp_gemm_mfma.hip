@@ -617,6 +617,15 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     const int e16 = ln & 15, eq = ln >> 4;
 #pragma unroll
     for (int qt = 0; qt < 4; ++qt) {
+      [[maybe_unused]] float sc[4];          // DX: the rows' places and scales, requested together
+      [[maybe_unused]] int to[4];
+      if constexpr (EPI == EPI_HEAD_DX)
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+          const int at = he.i0 + max(min(m0 + wm * 128 + qt * 32 + 8 * it + (ln >> 3), live - 1), 0);
+          sc[it] = he.scale[at];
+          to[it] = he.rows[at];
+        }
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -636,10 +645,9 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         if (grow < 0 || grow >= (SWAP ? he.out_rows : live) || gcol >= cols) continue;
         size_t off;
         if constexpr (EPI == EPI_HEAD_DX) {
-          const float sc = he.scale[he.i0 + grow];
-          off = (size_t)he.rows[he.i0 + grow] * ldc + gcol;
+          off = (size_t)to[it] * ldc + gcol;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= sc;
+          for (int e = 0; e < 8; ++e) v[e] *= sc[it];
         } else {
           off = (size_t)grow * ldc + gcol;
           if (he.add) {

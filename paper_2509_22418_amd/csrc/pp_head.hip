@@ -269,30 +269,72 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
   }
 }
 
+// 16 bytes at any element: the card loads and stores them in one go at any address
+struct __attribute__((packed, aligned(2))) any16 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(2))) any8 { uint32_t w[2]; };
+// columns c .. c + 3 of a row of d, those there are
+__device__ __forceinline__ float4 load_cols(const float* row, int c, int d) {
+  if (c + 4 <= d) {
+    const any16 r = *reinterpret_cast<const any16*>(row + c);
+    return make_float4(__uint_as_float(r.w[0]), __uint_as_float(r.w[1]), __uint_as_float(r.w[2]), __uint_as_float(r.w[3]));
+  }
+  return make_float4(c < d ? row[c] : 0.f, c + 1 < d ? row[c + 1] : 0.f, c + 2 < d ? row[c + 2] : 0.f, 0.f);
+}
+__device__ __forceinline__ void store_cols(float* row, int c, int d, const float4& v) {
+  if (c + 4 <= d) *reinterpret_cast<any16*>(row + c) = any16{{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)}};
+  else {
+    if (c < d) row[c] = v.x;
+    if (c + 1 < d) row[c + 1] = v.y;
+    if (c + 2 < d) row[c + 2] = v.z;
+  }
+}
+__device__ __forceinline__ void store_cols(bf16_t* row, int c, int d, const float4& v) {
+  if (c + 4 <= d) *reinterpret_cast<any8*>(row + c) = any8{{f32x2_to_bf16x2(v.x, v.y), f32x2_to_bf16x2(v.z, v.w)}};
+  else {
+    if (c < d) row[c] = from_f32<bf16_t>(v.x);
+    if (c + 1 < d) row[c + 1] = from_f32<bf16_t>(v.y);
+    if (c + 2 < d) row[c + 2] = from_f32<bf16_t>(v.z);
+  }
+}
+
 // Compact, padded copy of the rows that count; zeros behind them up to the last row of the copy; the outputs of rows that are left out.  A wave per row.
-template <class T>
-__global__ __launch_bounds__(256) void head_gather_kernel(const T* __restrict__ x, int ldx, T* __restrict__ xc, int dp, int d, const int32_t* __restrict__ pos, const int32_t* __restrict__ count,
-                                                          int n, int np, T* __restrict__ dx, int lddx, float* __restrict__ row_loss, float* __restrict__ row_lse) {
+__global__ __launch_bounds__(256) void head_gather_kernel(const float* __restrict__ x, int ldx, float* __restrict__ xc, int dp, int d, const int32_t* __restrict__ pos, const int32_t* __restrict__ count,
+                                                          int n, int np, float* __restrict__ dx, int lddx, float* __restrict__ row_loss, float* __restrict__ row_lse) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= np) return;
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
   if (t >= *count)
-    for (int c = lane; c < dp; c += 64) xc[(size_t)t * dp + c] = from_f32<T>(0.f);
+    for (int c = 4 * lane; c < dp; c += 256) *reinterpret_cast<float4*>(xc + (size_t)t * dp + c) = zero;
   if (t >= n) return;
   const int i = pos[t];
   if (i < 0) {
-    if (dx) for (int c = lane; c < d; c += 64) dx[(size_t)t * lddx + c] = from_f32<T>(0.f);
+    if (dx) for (int c = 4 * lane; c < d; c += 256) store_cols(dx + (size_t)t * lddx, c, d, zero);
     if (lane == 0) { row_loss[t] = 0.f; if (row_lse) row_lse[t] = 0.f; }
     return;
   }
-  for (int c = lane; c < dp; c += 64) xc[(size_t)i * dp + c] = c < d ? x[(size_t)t * ldx + c] : from_f32<T>(0.f);
+#pragma unroll 4
+  for (int c = 4 * lane; c < dp; c += 256) *reinterpret_cast<float4*>(xc + (size_t)i * dp + c) = load_cols(x + (size_t)t * ldx, c, d);
 }
 
-// dst [rows x ld_dst] = src [rows x cols], zeros from column cols to ld_dst
-template <class T>
-__global__ __launch_bounds__(256) void head_pad_kernel(const T* __restrict__ src, int ld_src, T* __restrict__ dst, int ld_dst, int rows, int cols) {
+// dst [rows x ld_dst] = src [rows x cols], zeros from column cols to ld_dst, a multiple of 8; dst 16-byte aligned.  A wave per row.
+__global__ __launch_bounds__(256) void head_pad_kernel(const bf16_t* __restrict__ src, int ld_src, bf16_t* __restrict__ dst, int ld_dst, int rows, int cols) {
   const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= rows) return;
-  for (int c = threadIdx.x & 63; c < ld_dst; c += 64) dst[(size_t)r * ld_dst + c] = c < cols ? src[(size_t)r * ld_src + c] : from_f32<T>(0.f);
+  const bf16_t* from = src + (size_t)r * ld_src;
+#pragma unroll 4
+  for (int c = (threadIdx.x & 63) * 8; c < ld_dst; c += 512) {
+    uint4 v;
+    if (c + 8 <= cols) {
+      const any16 u = *reinterpret_cast<const any16*>(from + c);
+      v = make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
+    } else {
+      uint32_t w[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w[k] = c + k < cols ? from[c + k].bits : 0;
+      v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    }
+    *reinterpret_cast<uint4*>(dst + (size_t)r * ld_dst + c) = v;
+  }
 }
 // dst[c][r] = src[r][c] for r < rows, zeros for rows <= r < ld_dst
 template <class T>
@@ -792,11 +834,10 @@ template <class T> struct FewChunk;          // 16 bytes of a row: 8 bf16 or 4 f
 template <> struct FewChunk<bf16_t> { static constexpr int E = 8; };
 template <> struct FewChunk<float> { static constexpr int E = 4; };
 
-struct __attribute__((packed, aligned(2))) few_raw { uint32_t w[4]; };          // 16 bytes at any element: the card loads them in one go from any address
 template <class T> __device__ __forceinline__ uint4 few_load(const T* row, int k, int d) {          // elements k .. of a row, zeros from d on
   constexpr int E = FewChunk<T>::E;
   if (k + E <= d) {
-    const few_raw r = *reinterpret_cast<const few_raw*>(row + k);
+    const any16 r = *reinterpret_cast<const any16*>(row + k);
     return make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
   }
   if (k >= d) return make_uint4(0, 0, 0, 0);
@@ -806,12 +847,12 @@ template <class T> __device__ __forceinline__ uint4 few_load(const T* row, int k
   return r.u;
 }
 __device__ __forceinline__ void few_load8(const bf16_t* p, float v[8]) {
-  const few_raw r = *reinterpret_cast<const few_raw*>(p);
+  const any16 r = *reinterpret_cast<const any16*>(p);
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r.w[i] << 16); v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u); }
 }
 __device__ __forceinline__ void few_load8(const float* p, float v[8]) {
-  const few_raw a = *reinterpret_cast<const few_raw*>(p), b = *reinterpret_cast<const few_raw*>(p + 4);
+  const any16 a = *reinterpret_cast<const any16*>(p), b = *reinterpret_cast<const any16*>(p + 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) { v[i] = __uint_as_float(a.w[i]); v[4 + i] = __uint_as_float(b.w[i]); }
 }
@@ -1094,41 +1135,45 @@ __global__ __launch_bounds__(256) void head_few_dw_kernel(HeadFew h, int cols) {
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
-// dx[rows[i]] = scale[i] (1 without) sum of the partials [splits][pitch][d], a wave per compact row of the piece; pitch 0: the rows that count, in whole groups of 64
+// Sum of the partials [splits][pitch] at one place of four columns, in their order, eight loads in flight
+__device__ __forceinline__ float4 sum_partials(const float* part, int splits, size_t pitch, int c, int d) {
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int z = 0; z < splits; z += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = z + k < splits ? load_cols(part + (z + k) * pitch, c, d) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { s.x += v[k].x; s.y += v[k].y; s.z += v[k].z; s.w += v[k].w; }
+  }
+  return s;
+}
+// A row takes as many lanes of a wave as it has groups of four columns, 1 << lg, and up to 64: narrow rows share a wave.
+static int row_lanes(int d) { int lg = 0; while (lg < 6 && (4 << lg) < d) ++lg; return lg; }
+static dim3 row_grid(int rows, int d) { const int per = 256 >> row_lanes(d); return dim3((rows + per - 1) / per, (d + 255) / 256); }
+// dx[rows[i]] = scale[i] (1 without) sum of the partials [splits][pitch][d] for the compact rows of the piece; pitch 0: the rows that count, in whole groups of 64
 template <class T>
 __global__ __launch_bounds__(256) void head_dx_sum_kernel(const float* __restrict__ part, int splits, const int32_t* __restrict__ splits_dev, int pitch, const float* __restrict__ scale, T* __restrict__ dx, int lddx, int d,
-                                                          const int32_t* __restrict__ rows, const int32_t* __restrict__ count, int i0, int piece) {
-  const int i = blockIdx.x * 4 + (threadIdx.x >> 6), live = min(max(*count - i0, 0), piece);
-  if (i >= live) return;
+                                                          const int32_t* __restrict__ rows, const int32_t* __restrict__ count, int i0, int piece, int lg) {
+  const int i = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), live = min(max(*count - i0, 0), piece), c = blockIdx.y * 256 + (threadIdx.x & ((1 << lg) - 1)) * 4;
+  if (i >= live || c >= d) return;
   if (splits_dev) { splits = *splits_dev; if (splits == 1) return; }          // then the product's own kernel wrote dx
-  const size_t mn = (size_t)(pitch ? pitch : (live + 63) & ~63) * d;
   const float sc = scale ? scale[i0 + i] : 1.f;
   const int t = rows[i0 + i];
-  for (int c = threadIdx.x & 63; c < d; c += 64) {
-    float s = 0.f;
-    int z = 0;
-    for (; z + 4 <= splits; z += 4) {          // four loads in flight
-      float v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = part[(z + k) * mn + (size_t)i * d + c];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s += v[k];
-    }
-    for (; z < splits; ++z) s += part[z * mn + (size_t)i * d + c];
-    dx[(size_t)t * lddx + c] = from_f32<T>(s * sc);
-  }
+  float4 s = sum_partials(part + (size_t)i * d, splits, (size_t)(pitch ? pitch : (live + 63) & ~63) * d, c, d);
+  s.x *= sc; s.y *= sc; s.z *= sc; s.w *= sc;
+  store_cols(dx + (size_t)t * lddx, c, d, s);
 }
 // out = sum of the partials [splits][rows][d] (+ add), out float or bf16
 template <class TO>
-__global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restrict__ part, int splits, const float* add, int ldadd, TO* out, int ldo, int rows, int d) {
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows) return;
-  for (int c = threadIdx.x & 63; c < d; c += 64) {
-    float s = 0.f;
-    for (int z = 0; z < splits; ++z) s += part[(size_t)z * rows * d + (size_t)r * d + c];
-    if (add) s += add[(size_t)r * ldadd + c];
-    out[(size_t)r * ldo + c] = from_f32<TO>(s);
+__global__ __launch_bounds__(256) void head_dw_sum_kernel(const float* __restrict__ part, int splits, const float* add, int ldadd, TO* out, int ldo, int rows, int d, int lg) {
+  const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), c = blockIdx.y * 256 + (threadIdx.x & ((1 << lg) - 1)) * 4;
+  if (r >= rows || c >= d) return;
+  float4 s = sum_partials(part + (size_t)r * d, splits, (size_t)rows * d, c, d);
+  if (add) {
+    const float4 a = load_cols(add + (size_t)r * ldadd, c, d);
+    s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
   }
+  store_cols(out + (size_t)r * ldo, c, d, s);
 }
 template <class TO>
 __global__ __launch_bounds__(256) void head_zero_kernel(TO* out, int ldo, int rows, int d) {
@@ -1203,7 +1248,7 @@ static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
     else head_row_kernel<1024, 0><<<m, 1024, 0, st>>>(z, g, h);
     if (a.dx) {
       k_gemm_nt_f32(st, 0, z, p.vp, wt, ldwt, part, a.d, m, a.d, p.vp, EPI_STORE, nullptr, 1, p.dx_splits, part, count, i0, m);
-      head_dx_sum_kernel<float><<<quads(m), 256, 0, st>>>(part, p.dx_splits, nullptr, m, nullptr, (float*)a.dx, a.lddx, a.d, rows, count, i0, m);
+      head_dx_sum_kernel<float><<<row_grid(m, a.d), 256, 0, st>>>(part, p.dx_splits, nullptr, m, nullptr, (float*)a.dx, a.lddx, a.d, rows, count, i0, m, row_lanes(a.d));
     }
     if (a.dw) {
       // (columns too long for the kernel's offsets cannot happen: vp < 2^20 + 128)
@@ -1213,7 +1258,7 @@ static void head_f32(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
       else {
         const int splits = m % (4 * p.dw_splits) == 0 ? p.dw_splits : 1;
         k_gemm_tn_f32(st, z + a.dw_lo, p.vp, dw_rows, 0, xp, p.dp, part, a.d, dw_rows, a.d, m, splits, part, count, i0, m);
-        head_dw_sum_kernel<float><<<quads(dw_rows), 256, 0, st>>>(part, splits, add ? dw : nullptr, a.lddw, dw, a.lddw, dw_rows, a.d);
+        head_dw_sum_kernel<float><<<row_grid(dw_rows, a.d), 256, 0, st>>>(part, splits, add ? dw : nullptr, a.lddw, dw, a.lddw, dw_rows, a.d, row_lanes(a.d));
       }
     }
   }
@@ -1268,7 +1313,7 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
       if (p.dx_whole) ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
       if (p.dx_splits > 1) {
         ok &= k_head_gemm(st, EPI_HEAD_PART, e, p.vp, w, ldw, part, a.d, m, a.d, p.vp, a.vocab, p.dx_splits, he) == 0;
-        head_dx_sum_kernel<bf16_t><<<quads(m), 256, 0, st>>>(part, 0, he.splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m);
+        head_dx_sum_kernel<bf16_t><<<row_grid(m, a.d), 256, 0, st>>>(part, 0, he.splits, 0, scale, (bf16_t*)a.dx, a.lddx, a.d, rows, count, i0, m, row_lanes(a.d));
       }
     }
     if (a.dw) {
@@ -1289,8 +1334,8 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
         ok &= k_head_gemm(st, EPI_HEAD_DW, xt, p.piece, e + v0, p.vp, out, ldo, a.d, a.dw_hi - v0, m, m, 1, he) == 0;
       else {
         ok &= k_head_gemm(st, EPI_HEAD_DW_PART, xt, p.piece, e + v0, p.vp, part, a.d, a.d, a.dw_hi - v0, m, m, p.dw_splits, he) == 0;
-        if (he.out_f32) head_dw_sum_kernel<float><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (float*)out, ldo, dw_rows, a.d);
-        else head_dw_sum_kernel<bf16_t><<<quads(dw_rows), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (bf16_t*)out, ldo, dw_rows, a.d);
+        if (he.out_f32) head_dw_sum_kernel<float><<<row_grid(dw_rows, a.d), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (float*)out, ldo, dw_rows, a.d, row_lanes(a.d));
+        else head_dw_sum_kernel<bf16_t><<<row_grid(dw_rows, a.d), 256, 0, st>>>(part, p.dw_splits, he.add, ldacc, (bf16_t*)out, ldo, dw_rows, a.d, row_lanes(a.d));
       }
     }
   }
@@ -1315,11 +1360,11 @@ int k_head(hipStream_t st, const HeadArgs& a, char* ws) {
   head_scan_kernel<<<1, 1024, 0, st>>>(a.targets, flags, a.row_weight, a.n, a.vocab, pos, rows, count, (int32_t*)(ws + p.redo), p.n_redo,
                                       a.dtype && a.dx ? (p.np + p.piece - 1) / p.piece : 0, p.piece, (a.d + 255) / 256, p.vp / 64, p.dx_splits, a.part_cap, a.d);
   if (a.dtype == 0)
-    head_gather_kernel<float><<<quads(p.np), 256, 0, st>>>((const float*)a.x, a.ldx, (float*)xc, p.dp, a.d, pos, count, a.n, p.np, (float*)a.dx, a.lddx, row_loss, a.row_lse);
+    head_gather_kernel<<<quads(p.np), 256, 0, st>>>((const float*)a.x, a.ldx, (float*)xc, p.dp, a.d, pos, count, a.n, p.np, (float*)a.dx, a.lddx, row_loss, a.row_lse);
   const void* w = a.w;
   int ldw = a.ldw;
   if (p.copy_w) {
-    PP_H_DISPATCH(a.dtype, head_pad_kernel<T><<<quads(a.vocab), 256, 0, st>>>((const T*)a.w, a.ldw, (T*)(ws + p.wc), p.dp, a.vocab, a.d));
+    head_pad_kernel<<<quads(a.vocab), 256, 0, st>>>((const bf16_t*)a.w, a.ldw, (bf16_t*)(ws + p.wc), p.dp, a.vocab, a.d);
     w = ws + p.wc; ldw = p.dp;
   }
   const void* wt = a.wt;
