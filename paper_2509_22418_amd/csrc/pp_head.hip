@@ -944,19 +944,25 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
       }
     }
     soft = __ballot(id[0] >= 0 || id[1] >= 0) != 0;
-    // at most 2048 partial sums, 32 a lane: all of them requested at once, the maximum first, then sums that do not wait for each other
+    // at most 2048 partial sums, 32 a lane: the maximum first, then sums that do not wait for each other; 16 loads in flight
     const float4* part = reinterpret_cast<const float4*>(h.part) + (size_t)t * h.parts;
-    constexpr int K = 2048 / 64;
-    float4 p[K];
+    for (int k0 = lane; k0 < h.parts; k0 += 16 * 64) {
+      float v[16];
 #pragma unroll
-    for (int k = 0; k < K; ++k) p[k] = lane + 64 * k < h.parts ? part[lane + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      for (int k = 0; k < 16; ++k) v[k] = k0 + 64 * k < h.parts ? part[k0 + 64 * k].x : -INFINITY;
 #pragma unroll
-    for (int k = 0; k < K; ++k) m = fmaxf(m, p[k].x);
+      for (int k = 0; k < 16; ++k) m = fmaxf(m, v[k]);
+    }
     m = wave_max(m);
+    for (int k0 = lane; k0 < h.parts; k0 += 16 * 64) {
+      float4 p[16];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      s += p[k].x == -INFINITY ? p[k].y : p[k].y * expf(p[k].x - m);          // a part without a finite logit has a sum of 0, or NaN
-      if (it != 1.f) s2 += p[k].x == -INFINITY ? p[k].z : p[k].z * expf((p[k].x - m) * it);
+      for (int k = 0; k < 16; ++k) p[k] = k0 + 64 * k < h.parts ? part[k0 + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        s += p[k].x == -INFINITY ? p[k].y : p[k].y * expf(p[k].x - m);          // a part without a finite logit has a sum of 0, or NaN
+        if (it != 1.f) s2 += p[k].x == -INFINITY ? p[k].z : p[k].z * expf((p[k].x - m) * it);
+      }
     }
     s = wave_sum(s);
     s2 = it == 1.f ? s : wave_sum(s2);
@@ -1025,8 +1031,9 @@ template <int NT>
 __device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float (*dz)[128]) {
   const float it = 1.0f / h.tau;
   __syncthreads();
-  for (int i = threadIdx.x; i < NT * 128; i += 256) {
-    const int t = i >> 7, r = i & 127;
+  const int lg = 32 - __clz(max(rows - 1, 1)), all = NT << lg;          // 2 ^ lg >= rows
+  for (int i = threadIdx.x; i < all; i += 256) {
+    const int t = i >> lg, r = i & ((1 << lg) - 1);
     float v = 0.f;
     if (t < h.n && r < rows) {
       const float4 c = *reinterpret_cast<const float4*>(h.coef + t * 4);
@@ -1092,7 +1099,13 @@ __global__ __launch_bounds__(1024) void head_few_sum_kernel(HeadFew h, int parti
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = blockIdx.y, c = blockIdx.x * 64 + lane;
   float s = 0.f;
   if (c < h.d)
-    for (int p = wave; p < partials; p += 16) s += h.psum[((size_t)p * h.n + t) * h.d + c];
+    for (int p = wave; p < partials; p += 8 * 16) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p + 16 * k < partials ? h.psum[((size_t)(p + 16 * k) * h.n + t) * h.d + c] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
   s_s[wave][lane] = s;
   __syncthreads();
   if (wave || c >= h.d) return;
