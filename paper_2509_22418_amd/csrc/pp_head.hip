@@ -379,7 +379,7 @@ __device__ __forceinline__ void head_entries(const HeadRow& h, int t, int* id_s,
   __syncthreads();
 }
 
-// BS threads, NV groups of four logits a thread held in registers (0: the row is read again for each pass).  One read and one write of the row where it fits.
+// BS threads, NV groups of four logits a thread held in registers (0: the row is read for the sums and again for dz; 16 groups would spill).  One read and one write of the row where it fits.
 template <int BS, int NV>
 __global__ __launch_bounds__(BS) void head_row_kernel(float* z_, int grads, HeadRow h) {
   __shared__ float red[17];
@@ -409,15 +409,34 @@ __global__ __launch_bounds__(BS) void head_row_kernel(float* z_, int grads, Head
 #pragma unroll
     for (int k = 0; k < NV; ++k) r[k] = fetch(tid + BS * k);
   }
-  float m = -INFINITY;
-  each([&](int, const float4& v) { m = fmaxf(fmaxf(m, fmaxf(v.x, v.y)), fmaxf(v.z, v.w)); });
-  m = block_max(m, red);
-  float s1 = 0.f, st = 0.f;
+  float m = -INFINITY, s1 = 0.f, st = 0.f;
   const bool two = h.tau != 1.f;
-  each([&](int, const float4& v) {
-    s1 += expf(v.x - m) + expf(v.y - m) + expf(v.z - m) + expf(v.w - m);
-    if (two) st += expf((v.x - m) * it) + expf((v.y - m) * it) + expf((v.z - m) * it) + expf((v.w - m) * it);
-  });
+  auto sums = [&](const float4& v, float top) {
+    s1 += expf(v.x - top) + expf(v.y - top) + expf(v.z - top) + expf(v.w - top);
+    if (two) st += expf((v.x - top) * it) + expf((v.y - top) * it) + expf((v.z - top) * it) + expf((v.w - top) * it);
+  };
+  auto largest = [](float m, const float4& v) { return fmaxf(fmaxf(m, fmaxf(v.x, v.y)), fmaxf(v.z, v.w)); };
+  if constexpr (NV > 0) {
+    each([&](int, const float4& v) { m = largest(m, v); });
+    m = block_max(m, red);
+    each([&](int, const float4& v) { sums(v, m); });
+  } else {          // one read for both: a thread's sums are against the largest logit it has seen
+    float mine = -INFINITY;
+    each([&](int, const float4& v) {
+      const float top = largest(mine, v);
+      if (top > mine) {
+        s1 *= expf(mine - top);
+        if (two) st *= expf((mine - top) * it);
+        mine = top;
+      }
+      if (mine != -INFINITY) sums(v, mine);
+      else s1 += v.x + v.y + v.z + v.w != -INFINITY ? NAN : 0.f;          // nothing but -inf and NaN so far: NaN has to reach the sum
+    });
+    m = block_max(mine, red);
+    const float back = mine == -INFINITY ? 1.f : expf(mine - m);
+    s1 *= back;
+    if (two) st *= mine == -INFINITY ? 1.f : expf((mine - m) * it);
+  }
   s1 = block_sum(s1, red);
   st = two ? block_sum(st, red) : s1;
   if (soft) head_entries(h, t, id_s, q_s, red);

@@ -277,6 +277,21 @@ def test_rows_far_apart_in_memory(n, dtype):
     check(call(far_x, far_w, y, dw=(1, 69)), x, w, y, dw=(1, 69))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["ce", "mixed"])
+def test_rows_wider_than_a_workgroup_holds(kind, dtype):
+    """Vocabularies beyond 32768: fp32 rows of logits that do not fit a workgroup's registers; their largest logits first, last and in the middle."""
+    n, vocab, d = 40, 50001, 64
+    k = dict(KINDS[kind])
+    x, w, y, ids, u = make(n, vocab, d, TYPES[dtype], top=k.pop("top"), std=2.0)
+    w[0], w[vocab - 1], w[30000] = 3 * w[0], 4 * w[vocab - 1], 5 * w[30000]
+    a = dict(ids=ids, u=u, **k) if ids is not None else {}
+    check(call(x, w, y, dw=(49000, vocab), **a), x, w, y, dw=(49000, vocab), **a)
+    x[3] = torch.nan
+    bad = call(x, w, y.clamp(min=0), **a)
+    assert np.isnan(bad["row_loss"][3]) and np.isnan(bad["dx"][3]).all() and not np.isnan(bad["dx"][[2, 4]]).any()
+
+
 def test_non_finite_rows_that_count_stay_in_their_rows():
     """NaN in a row that counts: its loss and its dX row are NaN, the other rows' are as without it."""
     x, w, y, _, _ = make(300, 500, 64, torch.bfloat16, ignored=0.0)
