@@ -468,13 +468,12 @@ int k_gemm_nt_ring(hipStream_t st, const void* A, int lda, const void* B, int ld
 
 // ---- exponentials of the output head's logits on 64 x 64 and 128 x 128 tiles
 // Which: by what the parts of a launch take (kTiles' steps; an epilogue of 3 / 5 us; a 256 x 256 tile 1.6 us a step and 8 us besides), for rounds of 256 units.
-int head_exp_ring(int M, int N, int K) {
-  const int steps = K / 64;
-  auto tiles = [&](int b) { return (long)((M + b - 1) / b) * ((N + b - 1) / b); };
-  const long big = (tiles(256) + 255) / 256 * (1600l * steps + 8000);
-  const long t128 = (tiles(128) + 255) / 256 * (493l * steps + 5000), t64 = (tiles(64) + 511) / 512 * (tiles(64) > 256 ? 371l * steps + 4000 : 216l * steps + 3000);
-  if (std::min(t128, t64) >= big) return 0;
-  return t64 < t128 ? 64 : 128;
+double head_exp_us(int M, int N, int K, int tile) {
+  const int steps = K / 64, b = tile ? tile : 256;
+  const long tiles = (long)((M + b - 1) / b) * ((N + b - 1) / b);
+  if (tile == 128) return (tiles + 255) / 256 * (0.493 * steps + 5);
+  if (tile == 64) return (tiles + 511) / 512 * (tiles > 256 ? 0.371 * steps + 4 : 0.216 * steps + 3);
+  return (tiles + 255) / 256 * (1.6 * steps + 8);
 }
 template <int B, int WM, int WN, bool WHOLE>
 static int launch_exp(hipStream_t st, const void* A, int lda, const void* Bp, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he) {

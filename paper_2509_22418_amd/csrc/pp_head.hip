@@ -34,7 +34,7 @@ constexpr int kTopMax = 128;          // entries per row (PP_HEAD_TOP_MAX)
 constexpr size_t kPieceBytes = 512ull << 20;
 struct HeadPlan {
   int dp, vp, np, piece, groups, exp_tile;          // padded width, padded vocabulary, rows of the compact X, rows of a piece, column groups of the first product's partial sums, its tile (0: 256)
-  int dx_splits, dw_splits, n_redo, parts;          // parts: waves of the first product of few rows (0: the other kernels)
+  int dx_splits, dw_splits, n_redo, ref_group, parts;          // ref_group: entries per wave of head_ref_kernel; parts: waves of the first product of few rows (0: the other kernels)
   bool grads, copy_w, own_wt, mixed, dx_whole, pick;          // pick: the first product picks the entries' logits
   size_t flags, pos, rows, count, rowl, ref, scale, coef, zsel, xc, wc, wt, z, stats, stats2, redo, offs, list, xt, part, dwa, total;          // byte offsets
 };
@@ -104,16 +104,23 @@ HeadPlan plan_head(const HeadArgs& a) {
   p.piece = a.piece ? pad_to(a.piece, 64) : std::max(256, (int)(limit / row / 256 * 256));
   // 2^18: grids of piece / 64 in y.  2 GiB: the products' 32-bit offsets and whatever a caller asks for
   p.piece = std::min({p.piece, p.np, 1 << 18, std::max(256, (int)((2ull << 30) / row / 256 * 256))});
-  // columns that one partial sum of a row covers, by the tiles of the first product; the last piece, which may be smaller, takes the tiles of the others
-  p.exp_tile = bf ? head_exp_ring(p.piece, a.vocab, p.dp) : 0;
-  const int wide = p.exp_tile ? p.exp_tile : 256;
+  if (bf) {
+    // The first product's tiles, and the logits of the teacher's entries: by dot products (head_ref_kernel: a row of W each, 7 TB/s out of the last-level cache, half a microsecond for each of a
+    // wave's ref_group), or picked from the accumulators of 256 x 256 tiles (the lists, and their look-ups in every tile; 8192 x 2048 x 32000 with 64 entries a row 315 us / 50 us).  The estimates,
+    // in us, are fitted to 165 shapes timed both ways (widths of 256 to 2048, 700 to 8000 rows, vocabularies of 8000 to 100000, 2 to 64 entries): on 159 the faster or one within 3 % of it is
+    // taken, on the others one within 7 %.  The last piece, which may be smaller, takes the tiles of the others.
+    // More waves with fewer entries each, where all rows' groups of 16 would be less than four waves a compute unit.
+    p.ref_group = 16;
+    while (p.ref_group > 4 && (long)p.np * ((a.top + p.ref_group - 1) / p.ref_group) < 1024) p.ref_group /= 2;
+    const double big = head_exp_us(p.piece, a.vocab, p.dp, 0), t128 = head_exp_us(p.piece, a.vocab, p.dp, 128), t64 = head_exp_us(p.piece, a.vocab, p.dp, 64);
+    const double rounds = (double)((p.piece + 255) / 256) * ((a.vocab + 255) / 256) / 256;
+    const double dots = a.top ? (double)p.piece * a.top * p.dp * 2 / 7e6 + std::min(a.top, p.ref_group) / 2. : 0;
+    const double picked = a.top && a.vocab <= 1 << 19 ? 6 + a.top / 12. + rounds * a.vocab / 9e4 : 1e30;          // (the lists' counters fit 32 KB of LDS)
+    p.pick = big + picked < std::min({big, t128, t64}) + dots;
+    p.exp_tile = p.pick || std::min(t128, t64) >= big ? 0 : t64 < t128 ? 64 : 128;
+  }
+  const int wide = p.exp_tile ? p.exp_tile : 256;          // columns that one partial sum of a row covers, by the tiles
   p.groups = (a.vocab + wide - 1) / wide * (wide / (p.exp_tile ? 32 : 64));
-  // Logits of the teacher's entries: by dot products (head_ref_kernel: a row of W each, 7 TB/s out of the last-level cache, half a microsecond for each of a wave's up to 16), or picked from the first
-  // product's accumulators (the lists, and their look-ups in every tile; 8192 x 2048 x 32000 with 64 entries a row 315 us / 50 us).  In us, fitted to 165 shapes timed both ways (widths of 256 to 2048, 700
-  // to 8000 rows, vocabularies of 8000 to 100000, 2 to 64 entries): on 159 the rule takes the faster or one within 3 % of it, on the others one within 7 %.
-  const double rounds = (double)((p.piece + 255) / 256) * ((a.vocab + 255) / 256) / 256;
-  p.pick = bf && a.top && !p.exp_tile && a.vocab <= 1 << 19 &&          // (the lists' counters fit 32 KB of LDS)
-           (double)p.piece * a.top * p.dp * 2 / 7e6 + std::min(a.top, 16) / 2. > 6 + a.top / 12. + rounds * a.vocab / 9e4;
   // the bf16 matrix kernels read rows that are multiples of 64 elements long, 16-byte aligned and not so far apart that the offsets among 64 of them pass 31 bits; the fp32 ones any
   p.copy_w = bf && (a.d % 64 || a.ldw % 8 || a.ldw > 1 << 22 || (uintptr_t)a.w & 15);
   p.own_wt = a.dx && !bf && !(a.wt && a.vocab % unit == 0);          // the bf16 products read W as it lies
@@ -489,7 +496,6 @@ struct HeadRef {
   const unsigned char* flags;
   float *zsel, *ref, *row_loss, *row_lse;
 };
-constexpr int kRefGroup = 16;
 __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= h.np) return;
@@ -1308,8 +1314,8 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
   bf16_t* e = p.grads ? (bf16_t*)(ws + p.z) : nullptr;
   const bf16_t* xc = (const bf16_t*)(ws + p.xc);
   bool ok = true;
-  const int group = p.pick ? 1 : kRefGroup;
-  head_ref_kernel<<<dim3((p.np + 3) / 4, p.pick ? 1 : std::max(1, (a.top + kRefGroup - 1) / kRefGroup)), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
+  const int group = p.pick ? 1 : p.ref_group;
+  head_ref_kernel<<<dim3((p.np + 3) / 4, p.pick ? 1 : std::max(1, (a.top + group - 1) / group)), 256, 0, st>>>(HeadRef{(const bf16_t*)a.x, (const bf16_t*)w, (bf16_t*)(ws + p.xc), (bf16_t*)a.dx, a.ldx, ldw, a.lddx, a.d, p.dp, a.n, p.np, a.vocab, a.top,
                                                        a.ldx % 8 == 0 && ((uintptr_t)a.x & 15) == 0, group, (const int32_t*)(ws + p.pos), count, a.targets, a.ids, a.logits, flags, zsel, ref, row_loss, a.row_lse});
   const float log2e = 1.44269504f;
   for (int i0 = 0; i0 < a.n; i0 += p.piece) {

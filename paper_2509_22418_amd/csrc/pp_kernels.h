@@ -182,8 +182,8 @@ __device__ __forceinline__ float head_exponent(uint32_t code) {
   if (code == 0xff7f) return -INFINITY;
   return code & 0x8000 ? (float)(0x8080 - 64 * 16 - (int)code) * 0.0625f : (float)((int)code - 0x0080) * (1.f / 256) - 64.f;
 }
-// The exponentials on the smaller-tile GEMM's tiles (he.tile); head_exp_ring: which pay for M rows at most, 0: none
-int head_exp_ring(int M, int N, int K);
+// Estimated time of the exponentials' product on 256 x 256 tiles (tile 0) or on the smaller-tile GEMM's (he.tile: 128, 64)
+double head_exp_us(int M, int N, int K, int tile);
 int k_head_exp_ring(hipStream_t st, const void* A, int lda, const void* B, int ldb, void* C, int ldc, int M, int N, int K, const HeadEpi& he);
 // Products on 256 x 256 tiles.  EPI_HEAD_EXP: A[M x K] B[N x K]^T, K-contiguous.  The others read B [K rows x ldb] as it lies, contraction index first:
 //   EPI_HEAD_DX, EPI_HEAD_PART     C[live x N] = A[live x K] B,   K a multiple of 64; rows of B from kreal on are not read (A's columns there are zeros)
