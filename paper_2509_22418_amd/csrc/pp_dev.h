@@ -43,6 +43,10 @@ __device__ __forceinline__ void store8(bf16_t* p, const float v[8]) {
   for (int i = 0; i < 4; ++i) w[i] = f32x2_to_bf16x2(v[2 * i], v[2 * i + 1]);
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
+// 16 and 8 bytes at any element: the card loads and stores them in one go at any address
+struct __attribute__((packed, aligned(2))) any16 { uint32_t w[4]; };
+struct __attribute__((packed, aligned(2))) any8 { uint32_t w[2]; };
+__device__ __forceinline__ any16 any_of(float a, float b, float c, float d) { return any16{{__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d)}}; }
 
 // logistic function and the SwiGLU product with the hardware reciprocal (1 ulp): shared by the stand-alone SwiGLU
 // kernels and the GEMM epilogue that fuses them, so that both paths give identical values

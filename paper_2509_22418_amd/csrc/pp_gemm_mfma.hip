@@ -652,11 +652,10 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
           off = (size_t)grow * ldc + gcol;
           if (he.add) {
             const float* ad = he.add + (size_t)grow * he.ldadd + gcol;
-            if (he.vec) {
-              float w[8];
-              load8(ad, w);
+            if (gcol + 8 <= cols) {
+              const any16 w0 = *reinterpret_cast<const any16*>(ad), w1 = *reinterpret_cast<const any16*>(ad + 4);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += w[e];
+              for (int e = 0; e < 4; ++e) { v[e] += __uint_as_float(w0.w[e]); v[4 + e] += __uint_as_float(w1.w[e]); }
             } else
 #pragma unroll
               for (int e = 0; e < 8; ++e)
@@ -665,14 +664,17 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         }
         if (EPI == EPI_HEAD_DW && he.out_f32) {
           float* o = reinterpret_cast<float*>(Cv) + off;
-          if (he.vec) store8(o, v);
-          else
+          if (gcol + 8 <= cols) {
+            *reinterpret_cast<any16*>(o) = any_of(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<any16*>(o + 4) = any_of(v[4], v[5], v[6], v[7]);
+          } else
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               if (gcol + e < cols) o[e] = v[e];
         } else {
           bf16_t* o = reinterpret_cast<bf16_t*>(Cv) + off;
-          if (he.vec) store8(o, v);
+          if (gcol + 8 <= cols)
+            *reinterpret_cast<any16*>(o) = any16{{f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]), f32x2_to_bf16x2(v[4], v[5]), f32x2_to_bf16x2(v[6], v[7])}};
           else
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -683,7 +685,6 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     stored = true;
   } else if constexpr (EPI == EPI_HEAD_DW_PART) {
     float* C = reinterpret_cast<float*>(Cv) + (size_t)z * (size_t)he.out_rows * (size_t)ldc;
-    const bool four = (ldc & 3) == 0 && (M & 3) == 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int row = n0 + wn * 64 + 16 * j + l16 - he.shift;
@@ -693,7 +694,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         const int col = m0 + wm * 128 + 16 * i + 4 * lq;
         if (col >= M) continue;
         float* o = C + (size_t)row * ldc + col;
-        if (four) *reinterpret_cast<float4*>(o) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+        if (col + 4 <= M) *reinterpret_cast<any16*>(o) = any_of(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
         else
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -918,7 +919,8 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
         float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
         if constexpr (OUT_F32) {
           float* C = reinterpret_cast<float*>(Cv) + (size_t)z * (size_t)M * (size_t)ldc + (size_t)row * ldc + col;
-          if (n_vec_ok) *reinterpret_cast<float4*>(C) = make_float4(v[0], v[1], v[2], v[3]);
+          if (EPI == EPI_HEAD_PART && col + 4 <= N) *reinterpret_cast<any16*>(C) = any_of(v[0], v[1], v[2], v[3]);
+          else if (n_vec_ok) *reinterpret_cast<float4*>(C) = make_float4(v[0], v[1], v[2], v[3]);
           else for (int e = 0; e < 4 && col + e < N; ++e) C[e] = v[e];
         } else {
           bf16_t* C = reinterpret_cast<bf16_t*>(Cv) + (size_t)row * ldc + col;

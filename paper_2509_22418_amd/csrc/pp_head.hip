@@ -62,10 +62,7 @@ int capped(int splits, double mn, size_t cap) {
 // Few rows: threads of a workgroup side by side (8 columns each), and rows of W per workgroup such that the workgroups' partial sums of dX are kFewPartials at most.
 constexpr int kFew = 16, kFewPartials = 512;
 int few_cols(int d) { int c = 1; while (c < 256 && c * 8 < d) c *= 2; return c; }
-int few_chunk(int rows, int d) {
-  const int groups = std::max(1, kFewPartials * few_cols(d) / 256);
-  return (rows + groups - 1) / groups;
-}
+int few_chunk(int rows, int d) { return std::max((rows + kFewPartials - 1) / kFewPartials, 2 * 256 / few_cols(d)); }          // two rows for every thread at least
 
 HeadPlan plan_head(const HeadArgs& a) {
   HeadPlan p{};
@@ -93,7 +90,7 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.zsel = take((size_t)kFew * (a.top + 1) * 4);
     if (a.dx) {
       const int chunk = few_chunk(a.vocab, a.d);
-      p.part = take((size_t)((a.vocab + chunk - 1) / chunk) * (256 / few_cols(a.d)) * a.n * a.d * 4);
+      p.part = take((size_t)((a.vocab + chunk - 1) / chunk) * a.n * a.d * 4);
     }
     p.total = off;
     return p;
@@ -276,9 +273,6 @@ __global__ __launch_bounds__(1024) void head_scan_kernel(const int32_t* __restri
   }
 }
 
-// 16 bytes at any element: the card loads and stores them in one go at any address
-struct __attribute__((packed, aligned(2))) any16 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(2))) any8 { uint32_t w[2]; };
 // columns c .. c + 3 of a row of d, those there are
 __device__ __forceinline__ float4 load_cols(const float* row, int c, int d) {
   if (c + 4 <= d) {
@@ -1108,14 +1102,37 @@ __global__ __launch_bounds__(256) void head_few_dx_kernel(HeadFew h, int cols) {
     for (; r + 3 * rp < rows; r += 4 * rp) { row(r); row(r + rp); row(r + 2 * rp); row(r + 3 * rp); }
     for (; r < rows; r += rp) row(r);
   }
-  if (c >= h.d) return;
-  float* out = h.psum + (size_t)(blockIdx.x * rp + rg) * h.n * h.d;
+  // The workgroup's sums of a column: lanes of a wave, then waves one after the other by way of shared memory, the last one stores
+  for (int o = cols; o < 64; o <<= 1)
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-    if (t < h.n)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < h.d) out[(size_t)t * h.d + c + e] = acc[t][e];
+      for (int e = 0; e < 8; ++e) acc[t][e] += __shfl_xor(acc[t][e], o, 64);
+  constexpr int HT = NT < 8 ? NT : 8;          // tokens at a time
+  __shared__ float red[HT][1024];
+  const int wave = threadIdx.x >> 6, rows_at = cols <= 64 ? wave : rg, last = cols <= 64 ? 3 : rp - 1;
+  const bool holds = cols >= 64 || (threadIdx.x & 63) < cols;
+  float* out = h.psum + (size_t)blockIdx.x * h.n * h.d;
+#pragma unroll
+  for (int t0 = 0; t0 < NT; t0 += HT)
+    for (int w = 0; w <= last; ++w) {
+      if (rows_at == w && holds)
+#pragma unroll
+        for (int t = 0; t < HT; ++t) {
+          float* at = &red[t][(cg * 8) & 1023];          // cols 256: one row at a time, nothing to add
+          if (w > 0)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[t0 + t][e] += at[e];
+          if (w < last)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) at[e] = acc[t0 + t][e];
+          else if (t0 + t < h.n)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (c + e < h.d) out[(size_t)(t0 + t) * h.d + c + e] = acc[t0 + t][e];
+        }
+      __syncthreads();
+    }
 }
 // dx = sum of the partials, a block per row and 64 columns, 16 waves of partials
 template <class T>
@@ -1247,7 +1264,7 @@ static void few_grads(hipStream_t st, const HeadArgs& a, HeadFew h) {
     h.chunk = few_chunk(a.vocab, a.d);
     const int groups = (a.vocab + h.chunk - 1) / h.chunk;
     head_few_dx_kernel<T, NT><<<dim3(groups, slices), 256, 0, st>>>(h, cols);
-    head_few_sum_kernel<T><<<dim3((a.d + 63) / 64, a.n), 1024, 0, st>>>(h, groups * (256 / cols));
+    head_few_sum_kernel<T><<<dim3((a.d + 63) / 64, a.n), 1024, 0, st>>>(h, groups);
   }
   if (a.dw) {
     const int rows = a.dw_hi - a.dw_lo;
@@ -1345,7 +1362,6 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
     }
     he.scale = scale; he.rows = rows;
     if (a.dx) {
-      he.vec = a.d % 8 == 0 && a.lddx % 8 == 0 && ((uintptr_t)a.dx & 15) == 0;
       he.ncols = p.dp;          // of W: d where that is a multiple of 64, else of its padded copy
       he.splits = (const int32_t*)(ws + p.redo) + p.n_redo + i0 / p.piece;
       if (p.dx_whole) ok &= k_head_gemm(st, EPI_HEAD_DX, e, p.vp, w, ldw, a.dx, a.lddx, m, a.d, p.vp, a.vocab, 1, he) == 0;
@@ -1367,7 +1383,6 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
       he.out_f32 = a.dw_f32 || !last;
       void* out = he.out_f32 ? (void*)acc : a.dw;
       const int ldo = he.out_f32 ? ldacc : a.lddw;
-      he.vec = a.d % 8 == 0 && ldo % 8 == 0 && (!he.add || ldacc % 8 == 0) && (((uintptr_t)out | (uintptr_t)he.add) & 15) == 0;
       if (p.dw_splits == 1)
         ok &= k_head_gemm(st, EPI_HEAD_DW, xt, p.piece, e + v0, p.vp, out, ldo, a.d, a.dw_hi - v0, m, m, 1, he) == 0;
       else {

@@ -168,7 +168,6 @@ struct HeadEpi {
   int shift, out_rows;
   const float* add;
   int ldadd, out_f32;
-  int vec;                         // DX, DW: rows of C (and add) are whole aligned groups of 8
 };
 // An exponent y <= 60 in 16 bits, for two softmaxes: each may need what the other's exponential has lost (exp(-100) is nothing in bf16, exp(-100 / 64) is not).  Steps of 2^-8 from -64 on
 // (exp2's relative error at most 2^-9 ln 2, less than the half step of a bf16 exponential), which is where the sharper softmax has its weight; below, down to -2096, steps of 2^-4: the
