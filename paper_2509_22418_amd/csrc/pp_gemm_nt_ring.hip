@@ -245,13 +245,23 @@ __global__ __launch_bounds__(64 * WM * WN, WHOLE ? 1 : NS == 2 ? 4 : 2) void gem
         const int grow = m0 + wm * TM + p * 32 + row, gcol = n0 + wn * TN + c * 8;
         float z[8], s = 0.f, s2 = 0.f, t = -INFINITY;
         load8(reinterpret_cast<const float*>(patch + row * PITCH + c * 32), z);
-        const float ref = he.ref[he.i0 + min(grow, M - 1)], off = -ref * he.k, off2 = -ref * he.kt, km = fmaxf(he.k, he.kt), offm = -ref * km;
+        float ref;
+        if (he.own) {
+          ref = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ref = fmaxf(ref, gcol + e < N ? z[e] : -INFINITY);
+#pragma unroll
+          for (int o = 1; o < PR; o <<= 1) ref = fmaxf(ref, __shfl_xor(ref, o, 64));
+          if (ref == -INFINITY) ref = 0.f;
+        } else
+          ref = he.ref[he.i0 + min(grow, M - 1)];
+        const float off = -ref * he.k, off2 = -ref * he.kt, km = fmaxf(he.k, he.kt), offm = -ref * km;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const bool in = gcol + e < N;
           const float y = in ? fmaf(z[e], he.k, off) : -INFINITY;
           const float ex = __builtin_amdgcn_exp2f(y);
-          t = fmaxf(t, y);
+          t = fmaxf(t, he.own && in ? z[e] : y);
           s += ex;
           if (he.kt != 0.f) {
             s2 += in ? __builtin_amdgcn_exp2f(fmaf(z[e], he.kt, off2)) : 0.f;

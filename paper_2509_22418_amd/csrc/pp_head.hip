@@ -628,9 +628,10 @@ struct HeadFin {
   bf16_t* e;                    // nullptr: losses alone
   int places;                   // 1: the places are written
   int32_t* redo;
-  float tau, share;
+  float tau, share, k, kt;          // k, kt: HeadEpi's
 };
 constexpr float kFar = 40.f;          // e <= exp(40): sums of 2^20 of them, times what dX's product adds up, stay far from overflow, and C far from underflow
+template <bool OWN>          // sums against the groups' own largest logits
 __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
   __shared__ float s1_s[64][17], s2_s[64][17], top_s[64][17];          // 17: columns on different banks
   __shared__ __align__(16) int id_s[16][kTopMax];
@@ -645,6 +646,14 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
     const float2* sp = h.stats + row;
     const float* sp2 = h.stats2 + row;
     int g = slice;
+    for (; OWN && g < h.groups; g += 64) {          // each group's sum to the largest logit so far
+      const float2 v = sp[(size_t)g * h.piece];
+      const float u = h.mixed ? sp2[(size_t)g * h.piece] : 0.f, m = fmaxf(far, v.y);
+      if (m == -INFINITY) { s1 += v.x; s2 += u; continue; }          // nothing, or NaN
+      s1 = s1 * __builtin_amdgcn_exp2f((far - m) * h.k) + v.x * __builtin_amdgcn_exp2f((v.y - m) * h.k);
+      s2 = s2 * __builtin_amdgcn_exp2f((far - m) * h.kt) + u * __builtin_amdgcn_exp2f((v.y - m) * h.kt);
+      far = m;
+    }
     for (; g + 7 * 64 < h.groups; g += 8 * 64) {          // eight loads in flight
       float2 v[8];
 #pragma unroll
@@ -671,19 +680,24 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
   if (b0 + wave >= live) return;
   {
     const int r = wave;          // a row per wave from here on
-    const float sa = wave_sum(s1_s[lane][r]), st = h.mixed ? wave_sum(s2_s[lane][r]) : sa;          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
     const float far = wave_max(top_s[lane][r]);
+    float sl = s1_s[lane][r], sl2 = s2_s[lane][r];
+    if (OWN && far != -INFINITY) {
+      sl *= __builtin_amdgcn_exp2f((top_s[lane][r] - far) * h.k);
+      sl2 *= __builtin_amdgcn_exp2f((top_s[lane][r] - far) * h.kt);
+    }
+    const float sa = wave_sum(sl), st = h.mixed ? wave_sum(sl2) : sa;          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
     // Largest exponent, in units of log 2 of the stored exponential; with two softmaxes the second's may be larger.  Such a row takes its maximum as reference (what the rest of this
     // kernel makes of it is overwritten when its block is done again).
     const float span = far * 0.693147181f * (h.mixed ? fmaxf(1.f, 1.f / h.tau) : 1.f);
-    if (!h.again && span > kFar && far < 1e30f && lane == 0) {
+    if (!OWN && !h.again && span > kFar && far < 1e30f && lane == 0) {
       h.ref[h.i0 + b0 + r] += far * 0.693147181f * (h.mixed ? 1.f : h.tau);
       h.redo[0] = 1;
       h.redo[1 + b0 / 256] = 1;
     }
     const int i = h.i0 + b0 + r, t = h.rows[i];
     const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
-    const float ref = h.ref[i], it = 1.0f / h.tau;
+    const float ref = OWN ? (far == -INFINITY ? 0.f : far) : h.ref[i], it = 1.0f / h.tau;
     const float* zs = h.zsel + (size_t)i * (h.top + 1);
     const int y = hard ? h.targets[t] : -1;
     const float zy = hard ? zs[h.top] : 0.f;
@@ -1346,19 +1360,24 @@ static bool head_bf16(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char
       head_lists_kernel<<<(m + 127) / 128, 1024, groups64 * 4, st>>>(rows, count, a.ids, a.logits, flags, a.vocab, a.top, i0, m, groups64, (int32_t*)(ws + p.offs), (int32_t*)(ws + p.list));
       he.offs = (const int32_t*)(ws + p.offs); he.list = (const int32_t*)(ws + p.list); he.zsel = zsel; he.top = a.top;
     }
+    he.own = !e && p.exp_tile;          // losses alone need no reference beforehand: no second launches (on 256 x 256 tiles the longer epilogue costs as much as those)
     HeadFin f{stats, stats2, p.groups, m, i0, a.vocab, p.vp, a.top, p.mixed, 0, rows, count, a.targets, a.ids, a.logits, a.row_weight, zsel, flags, ref, scale, row_loss, a.row_lse, coef, e,
-              !p.mixed, redo, a.tau, a.share};
+              !p.mixed, redo, a.tau, a.share, he.k, he.kt};
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
-    head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
+    if (he.own) {
+      head_fin_kernel<true><<<m / 16, 1024, 0, st>>>(f);
+      continue;
+    }
+    head_fin_kernel<false><<<m / 16, 1024, 0, st>>>(f);
     he.redo = redo; he.offs = nullptr;          // the logits are picked already
     f.again = 1;
     ok &= k_head_gemm(st, EPI_HEAD_EXP, xp, p.dp, w, ldw, e, p.vp, m, a.vocab, p.dp, p.dp, 1, he) == 0;
-    head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
+    head_fin_kernel<false><<<m / 16, 1024, 0, st>>>(f);
     if (!e) continue;
     if (p.mixed) {
       head_mix_kernel<<<dim3(m, (p.vp / 8 + 1023) / 1024), 256, 0, st>>>(e, p.vp, coef, count, i0, m, std::min(1.f, a.tau), std::min(1.f, 1.f / a.tau));
       f.again = 0; f.places = 1;
-      head_fin_kernel<<<m / 16, 1024, 0, st>>>(f);
+      head_fin_kernel<false><<<m / 16, 1024, 0, st>>>(f);
     }
     he.scale = scale; he.rows = rows;
     if (a.dx) {

@@ -151,6 +151,7 @@ struct HeadEpi {
   float* stats2;
   float k, kt;
   int tile;                        // 0: 256 x 256 tiles, groups of 64 columns; 128, 64: the smaller-tile GEMM's, groups of 32
+  int own;                         // 128, 64: sums against the largest of the group's own logits, which is stored with them, instead of ref
   int vp;
   // Entries whose logits are wanted (nullptr: none): those of rows 128 h .. and columns 64 g .. are list[128 h top + offs[h][g]] up to offs[h][g + 1] (pitch of offs: groups of 64 columns of the
   // tiles, plus one), each row in the 128 (7 bits), column in the 64 (6 bits), place j among the row's entries: z goes to zsel[row of all][j], rows of top + 1
