@@ -532,28 +532,37 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
     // sum / maximum over the four lanes that hold a row's columns: row swaps in registers instead of trips through LDS
     auto swap16 = [](float v) { return __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
     auto swap32 = [](float v) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
-    if (he.kt != 0.f) {          // two softmaxes: both sums, and the exponents in place of the logits
-      const float km = fmaxf(he.k, he.kt);
+    auto row_sum = [&](float v) {
+      const auto a = swap16(v);
+      const auto b = swap32(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+      return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    };
+    auto row_max = [&](float v) {
+      const auto a = swap16(v);
+      const auto b = swap32(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+      return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    };
+    if (he.kt != 0.f) {          // two softmaxes: both sums, and the sharper one's exponents in place of the logits
+      const bool swap = he.kt > he.k;
+      const float ks = swap ? he.kt : he.k, ko = swap ? he.k : he.kt;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float off = -rk[i] * he.k, off2 = -rk[i] * he.kt, offm = -rk[i] * km;
-        float s = 0.f, s2 = 0.f, t = -INFINITY;
+        const float offs = -rk[i] * ks, offo = -rk[i] * ko;
+        float s = 0.f, o = 0.f, t = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float z = acc[i][j][r], y = fmaf(z, he.k, off);
+            const float y = fmaf(acc[i][j][r], ks, offs);
             t = fmaxf(t, y);
             s += __builtin_amdgcn_exp2f(y);
-            s2 += __builtin_amdgcn_exp2f(fmaf(z, he.kt, off2));
-            acc[i][j][r] = head_exponent_code(fmaf(z, km, offm));
+            o += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], ko, offo));
+            acc[i][j][r] = head_exponent_code(y);
           }
-        s += __shfl_xor(s, 16, 64); s += __shfl_xor(s, 32, 64);
-        s2 += __shfl_xor(s2, 16, 64); s2 += __shfl_xor(s2, 32, 64);
-        t = fmaxf(t, __shfl_xor(t, 16, 64)); t = fmaxf(t, __shfl_xor(t, 32, 64));
+        s = row_sum(s); o = row_sum(o); t = row_max(t);
         if (eq == 0 && row0 + 16 * i < M) {
-          he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
-          he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = s2;
+          he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(swap ? o : s, t);
+          he.stats2[(size_t)grp * he.piece + row0 + 16 * i] = swap ? s : o;
         }
       }
     }
@@ -576,10 +585,7 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
             acc[i][j][r] = __builtin_amdgcn_exp2f(y);
             s += acc[i][j][r];
           }
-        const auto s16 = swap16(s), t16 = swap16(t);
-        s = __uint_as_float(s16[0]) + __uint_as_float(s16[1]); t = fmaxf(__uint_as_float(t16[0]), __uint_as_float(t16[1]));
-        const auto s32 = swap32(s), t32 = swap32(t);
-        s = __uint_as_float(s32[0]) + __uint_as_float(s32[1]); t = fmaxf(__uint_as_float(t32[0]), __uint_as_float(t32[1]));
+        s = row_sum(s); t = row_max(t);
         if (eq == 0 && row0 + 16 * i < M) he.stats[(size_t)grp * he.piece + row0 + 16 * i] = make_float2(s, t);
       }
       if (hi == 1 && has_next) {

@@ -255,19 +255,22 @@ __global__ __launch_bounds__(64 * WM * WN, WHOLE ? 1 : NS == 2 ? 4 : 2) void gem
           if (ref == -INFINITY) ref = 0.f;
         } else
           ref = he.ref[he.i0 + min(grow, M - 1)];
-        const float off = -ref * he.k, off2 = -ref * he.kt, km = fmaxf(he.k, he.kt), offm = -ref * km;
+        const float off = -ref * he.k, off2 = -ref * he.kt;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const bool in = gcol + e < N;
           const float y = in ? fmaf(z[e], he.k, off) : -INFINITY;
           const float ex = __builtin_amdgcn_exp2f(y);
-          t = fmaxf(t, he.own && in ? z[e] : y);
           s += ex;
           if (he.kt != 0.f) {
-            s2 += in ? __builtin_amdgcn_exp2f(fmaf(z[e], he.kt, off2)) : 0.f;
-            z[e] = head_exponent_code(in ? fmaf(z[e], km, offm) : -INFINITY);
-          } else
+            const float y2 = in ? fmaf(z[e], he.kt, off2) : -INFINITY, ys = he.kt > he.k ? y2 : y;
+            s2 += __builtin_amdgcn_exp2f(y2);
+            t = fmaxf(t, he.own && in ? z[e] : ys);
+            z[e] = head_exponent_code(ys);
+          } else {
+            t = fmaxf(t, he.own && in ? z[e] : y);
             z[e] = ex;
+          }
         }
 #pragma unroll
         for (int o = 1; o < PR; o <<= 1) { s += __shfl_xor(s, o, 64); t = fmaxf(t, __shfl_xor(t, o, 64)); s2 += __shfl_xor(s2, o, 64); }

@@ -687,11 +687,11 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
       sl2 *= __builtin_amdgcn_exp2f((top_s[lane][r] - far) * h.kt);
     }
     const float sa = wave_sum(sl), st = h.mixed ? wave_sum(sl2) : sa;          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
-    // Largest exponent, in units of log 2 of the stored exponential; with two softmaxes the second's may be larger.  Such a row takes its maximum as reference (what the rest of this
+    // Largest exponent, of the sharper one of two softmaxes, as a power of two.  Such a row takes its maximum as reference (what the rest of this
     // kernel makes of it is overwritten when its block is done again).
-    const float span = far * 0.693147181f * (h.mixed ? fmaxf(1.f, 1.f / h.tau) : 1.f);
+    const float span = far * 0.693147181f;
     if (!OWN && !h.again && span > kFar && far < 1e30f && lane == 0) {
-      h.ref[h.i0 + b0 + r] += far * 0.693147181f * (h.mixed ? 1.f : h.tau);
+      h.ref[h.i0 + b0 + r] += span * (h.mixed ? fminf(1.f, h.tau) : h.tau);
       h.redo[0] = 1;
       h.redo[1 + b0 / 256] = 1;
     }

@@ -144,7 +144,7 @@ struct HeadArgs {
 struct HeadEpi {
   const int32_t* count;
   int i0, piece;
-  // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and group of columns the sum of e, the largest exponent and, where kt != 0,
+  // EPI_HEAD_EXP: C = e = exp2(k (z - ref)) (nullptr: not stored), 0 in columns [N, vp); per row and group of columns the sum of e, the largest exponent (of max(k, kt)) and, where kt != 0,
   // the sum of exp2(kt (z - ref)), at [group][row of the piece].  Where kt != 0, C holds not e but the exponent max(k, kt) (z - ref) as head_exponent_code makes it.
   const float* ref;
   float2* stats;
@@ -175,8 +175,9 @@ struct HeadEpi {
 // sharper exponential is below 2^-64 there, and the softer's error is 2^-5 ln 2 over the ratio of the temperatures, on a weight of at most 2^(-64 / ratio).  The code is the upper half
 // of a normal float, so that rounding that float to bf16 stores it: 0x0080 + step, 0x8080 + step below -64, 0xff7f for nothing at all.
 __device__ __forceinline__ float head_exponent_code(float y) {
-  const float w = y + 64.f, steps = fminf(fmaxf(256.f * w, -16.f * w) + 128.5f, 0x7f7f);          // without a choice: the epilogues that call this have no registers for its masks
-  return __uint_as_float((uint32_t)steps << 16 | (__float_as_uint(w) & 0x80000000u));
+  // 2^23 added: the sum's rounding is the rounding to steps, which are its low bits.  No choice between the two: the epilogues that call this have no registers for its masks.
+  const float steps = fminf(fmaxf(fmaf(y, 256.f, 8388608.f + 128.f + 64.f * 256.f), fmaf(y, -16.f, 8388608.f + 128.f - 64.f * 16.f)), 8388608.f + 0x7f7f);
+  return __uint_as_float(__float_as_uint(steps) << 16 | (__float_as_uint(y + 64.f) & 0x80000000u));
 }
 __device__ __forceinline__ float head_exponent(uint32_t code) {
   if (code == 0xff7f) return -INFINITY;
