@@ -307,6 +307,14 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   auto load_lds = [&](uint32_t dst, uint32_t off, const char* base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "memory");
   };
+  // the same in assembly for kernels whose main loop loads by the builtin (every load of either kind sets m0 for itself)
+  [[maybe_unused]] auto issue_quiet = [&](const bf16_t* const (&g)[4], int s, int slot) {
+    const size_t koff = (size_t)max(min(s, ns - 1), 0) * DL_BK;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds0 + (slot * DL_UNIT_CHUNKS + wdst + i * 64) * 16)), "v"(g[i] + koff)
+                   : "memory");
+  };
   auto issueA = [&](int s, int slot) {
     if constexpr (BK_FIRST) {
       const char* b = baseA + (size_t)max(min(s, ns - 1), 0) * (DL_BK * 2);
@@ -364,7 +372,8 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   [[maybe_unused]] auto load_bounds = [&](int tm, int tn) {
     lo = hi_ = 0;
     if (tm * BM + wm * 128 >= M) return;          // there are lists for the 128-row halves that have rows
-    const int32_t* o = he.offs + (size_t)(tm * 2 + wm) * (tiles_n * 4 + 1) + tn * 4 + wn;
+    // read by way of the scalar cache (nothing writes them while this kernel runs): a vector load would be waited for with every load and store in front of it
+    const auto* o = (const __attribute__((address_space(4))) int32_t*)(he.offs + (size_t)(tm * 2 + wm) * (tiles_n * 4 + 1) + tn * 4 + wn);
     lo = o[0]; hi_ = o[1];
   };
   if constexpr (EXP) {
@@ -379,7 +388,6 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   const int m0 = tm * BM, n0 = tn * BN;
   [[maybe_unused]] int ent = 0;
   if constexpr (PICK) {
-      lo = __builtin_amdgcn_readfirstlane(lo); hi_ = __builtin_amdgcn_readfirstlane(hi_);
       if (lo + lane < hi_) ent = he.list[(size_t)(tm * 2 + wm) * 128 * he.top + lo + lane];
     }
   __builtin_amdgcn_s_barrier();
@@ -484,7 +492,11 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   if (has_next) {
     tile_of(vb_next, tm_next, tn_next);
     set_ptrs(tm_next, tn_next);
-    issueA(0, 0); issueB(0, 1); issueA(1, 2);
+    if constexpr (EXP) {          // in assembly as well: the compiler would wait for them in front of the epilogue's traffic with LDS (534 x 1856 x 122408 with picked logits 719 -> 686 us)
+      issue_quiet(gA, 0, 0); issue_quiet(gB, 0, 1); issue_quiet(gA, 1, 2);
+    } else {
+      issueA(0, 0); issueB(0, 1); issueA(1, 2);
+    }
   }
   __builtin_amdgcn_sched_barrier(0);
 
@@ -509,26 +521,29 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
             for (int i = 0; i < 8; ++i) acc[i][j][r] = -INFINITY;
     }
     const int row0 = m0 + wm * 128 + e16;
-    if (PICK && lo < hi_) {          // wanted logits, by way of the wave's patch: 32 rows of floats at a time (16-byte piece p of row r at p ^ (r & 15))
-      const int32_t* list = he.list + (size_t)(tm * 2 + wm) * 128 * he.top;
-      const size_t base = (size_t)(he.i0 + m0 + wm * 128);
+    if constexpr (PICK)          // wanted logits, 64 at a time, by way of the wave's patch: 32 rows of floats after another (16-byte piece p of row r at p ^ (r & 15)), every lane reads its
+      for (int at = lo; at < hi_; at += 64) {          // entry's place in each; LDS keeps the order of a wave's reads and writes, so that nothing waits before the end
+        const bool mine = at + ln < hi_;
+        const int row = ent & 127, c = (ent >> 7) & 63;
+        float got[4];
 #pragma unroll
-      for (int qt = 0; qt < 4; ++qt) {
-        if (hi_ - lo <= 64 && !__ballot(lo + ln < hi_ && ((ent >> 5) & 3) == qt)) continue;
+        for (int qt = 0; qt < 4; ++qt) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int row = x * 16 + e16;
-            *reinterpret_cast<float4*>(wbase + row * 256 + (((4 * j + eq) ^ (row & 15)) << 4)) = make_float4(acc[2 * qt + x][j][0], acc[2 * qt + x][j][1], acc[2 * qt + x][j][2], acc[2 * qt + x][j][3]);
-          }
-        for (int at = lo + ln; at < hi_; at += 64) {
-          const int en = at < lo + 64 ? ent : list[at], row = en & 127, c = (en >> 7) & 63;
-          if ((row >> 5) == qt)
-            he.zsel[(base + row) * (he.top + 1) + (en >> 13)] = *reinterpret_cast<const float*>(wbase + (row & 31) * 256 + (((c >> 2) ^ (row & 15)) << 4) + (c & 3) * 4);
+            for (int j = 0; j < 4; ++j) {
+              const int r = x * 16 + e16;
+              *reinterpret_cast<float4*>(wbase + r * 256 + (((4 * j + eq) ^ (r & 15)) << 4)) = make_float4(acc[2 * qt + x][j][0], acc[2 * qt + x][j][1], acc[2 * qt + x][j][2], acc[2 * qt + x][j][3]);
+            }
+          got[qt] = *reinterpret_cast<const float*>(wbase + (row & 31) * 256 + (((c >> 2) ^ (row & 15)) << 4) + (c & 3) * 4);
+        }
+        const float z = row & 64 ? (row & 32 ? got[3] : got[2]) : (row & 32 ? got[1] : got[0]);
+        if (mine) he.zsel[(size_t)(he.i0 + m0 + wm * 128 + row) * (he.top + 1) + (ent >> 13)] = z;
+        if (at + 64 < hi_) {          // waited for here: at the loop's head the first 64 would wait for the next tile's units too
+          ent = he.list[(size_t)(tm * 2 + wm) * 128 * he.top + min(at + 64 + ln, hi_ - 1)];
+          __builtin_amdgcn_s_waitcnt(0x0F70);
         }
       }
-    }
     // sum / maximum over the four lanes that hold a row's columns: row swaps in registers instead of trips through LDS
     auto swap16 = [](float v) { return __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
     auto swap32 = [](float v) { return __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false); };
