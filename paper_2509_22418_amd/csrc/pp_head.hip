@@ -1059,9 +1059,9 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
   }
 }
 
-// dz of rows v0 .. v0 + rows - 1 of W for NT tokens into shared memory; every thread calls it
+// dz[r][t] of rows v0 .. v0 + rows - 1 of W for NT tokens into shared memory; every thread calls it
 template <int NT>
-__device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float (*dz)[128]) {
+__device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float (*dz)[NT]) {
   const float it = 1.0f / h.tau;
   __syncthreads();
   const int lg = 32 - __clz(max(rows - 1, 1)), all = NT << lg;          // 2 ^ lg >= rows
@@ -1073,18 +1073,29 @@ __device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float
       const float a = h.z[(size_t)t * h.ldz + v0 + r] - c.x;
       if (c.w != 0.f) v = (c.y != 0.f ? c.y * expf(a) : 0.f) + (c.z != 0.f ? c.z * expf(a * it) : 0.f);
     }
-    dz[t][r] = v;
+    dz[r][t] = v;
   }
   __syncthreads();
   for (int i = threadIdx.x; i < h.n * (h.top + 1); i += 256) {          // no two entries of a row have the same place
     const int t = i / (h.top + 1), v = h.sid[i];
-    if (v >= v0 && v < v0 + rows) dz[t][v - v0] -= h.sub[i];
+    if (v >= v0 && v < v0 + rows) dz[v - v0][t] -= h.sub[i];
   }
   __syncthreads();
 }
+template <int NT> __device__ __forceinline__ void few_row(const float* dz, float g[NT]) {          // four tokens a read
+  if constexpr (NT % 4 == 0) {
+#pragma unroll
+    for (int t = 0; t < NT; t += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(dz + t);
+      g[t] = v.x; g[t + 1] = v.y; g[t + 2] = v.z; g[t + 3] = v.w;
+    }
+  } else
+#pragma unroll
+    for (int t = 0; t < NT; ++t) g[t] = dz[t];
+}
 // Threads of a workgroup: `cols` of them side by side, 8 columns each, 256 / cols rows of W at a time
 template <class T, int NT>
-__device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[128], float (*red)[1024]) {
+__device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[NT], float (*red)[1024]) {
   const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
   const int lo = blockIdx.x * h.chunk, hi = min(lo + h.chunk, h.V);
   float acc[NT][8];
@@ -1104,12 +1115,12 @@ __device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[1
       else
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < h.d ? to_f32(p[e]) : 0.f;
+      float g[NT];
+      few_row<NT>(dz[r], g);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float g = dz[t][r];
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[t][e] = fmaf(g, v[e], acc[t][e]);
-      }
+        for (int e = 0; e < 8; ++e) acc[t][e] = fmaf(g[t], v[e], acc[t][e]);
     };
     int r = rg;
     for (; r + 3 * rp < rows; r += 4 * rp) { row(r); row(r + rp); row(r + 2 * rp); row(r + 3 * rp); }
@@ -1167,7 +1178,7 @@ __global__ __launch_bounds__(1024) void head_few_sum_kernel(HeadFew h, int parti
   ((T*)h.dx)[(size_t)t * h.lddx + c] = from_f32<T>(h.coef[t * 4 + 3] != 0.f ? s : 0.f);
 }
 template <class T, class TO, int NT>
-__device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, float (*dz)[128]) {
+__device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, float (*dz)[NT]) {
   const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
   const int lo = h.dw_lo + group * h.chunk_dw, hi = min(lo + h.chunk_dw, h.dw_hi);
   float x[NT][8];
@@ -1181,12 +1192,12 @@ __device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, fl
     if (c >= h.d) continue;
     for (int r = rg; r < rows; r += rp) {
       float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      float g[NT];
+      few_row<NT>(dz[r], g);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float g = dz[t][r];
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(g, x[t][e], o[e]);
-      }
+        for (int e = 0; e < 8; ++e) o[e] = fmaf(g[t], x[t][e], o[e]);
       TO* p = (TO*)h.dw + (size_t)(v0 + r - h.dw_lo) * h.lddw + c;
       const bool whole = c + 8 <= h.d && h.lddw % 8 == 0 && ((uintptr_t)h.dw & 15) == 0;
       if (h.dw_add)
@@ -1203,7 +1214,8 @@ __device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, fl
 // The first `groups` workgroups form dX's partial sums, the others dW: neither waits for the other, so they share a launch (8 x 512 x 5000 60.6 -> 55.4 us, one row of 2048 x 32000 90 -> 81)
 template <class T, class TO, int NT>
 __global__ __launch_bounds__(256) void head_few_grads_kernel(HeadFew h, int cols, int groups) {
-  __shared__ float dz[NT][128], red[NT < 8 ? NT : 8][1024];
+  __shared__ __align__(16) float dz[128][NT];
+  __shared__ float red[NT < 8 ? NT : 8][1024];
   if ((int)blockIdx.x < groups) few_dx<T, NT>(h, cols, dz, red);
   else few_dw<T, TO, NT>(h, cols, blockIdx.x - groups, dz);
 }
@@ -1296,6 +1308,7 @@ static void head_few(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char*
   if (!a.dx && !a.dw) return;
   if (a.n == 1) few_grads<T, 1>(st, a, h);
   else if (a.n <= 4) few_grads<T, 4>(st, a, h);
+  else if (a.n <= 8) few_grads<T, 8>(st, a, h);
   else few_grads<T, 16>(st, a, h);
 }
 
