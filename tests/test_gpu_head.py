@@ -373,6 +373,49 @@ def test_captured_and_replayed(kind):
             assert np.array_equal(v.double().cpu().numpy(), ref[name]), (seed, name)
 
 
+@pytest.mark.parametrize("n,vocab,d,top,dtype,grads", [(3, 500, 72, 5, "bf16", True), (9, 500, 72, 0, "f32", False), (100, 300, 40, 4, "f32", True), (200, 700, 64, 6, "bf16", False), (2500, 3000, 128, 100, "bf16", True)])
+def test_two_captured_calls_share_a_workspace(n, vocab, d, top, dtype, grads):
+    """Few rows, fp32, losses alone and picked entries: two graphs over one workspace, replayed one after the other with eager calls in between."""
+    ins = [make(n, vocab, d, TYPES[dtype], top=top, seed=30 + i) for i in range(2)]
+    outs = [dict(loss=torch.empty(1, device="cuda"), row_loss=torch.empty(n, device="cuda"), row_lse=torch.empty(n, device="cuda"),
+                 **(dict(dx=torch.empty_like(i[0]), dw=torch.empty((vocab, d), device="cuda")) if grads else {})) for i in ins]
+    heads = [pp.make_head(i[0], i[1], **o) for i, o in zip(ins, outs)]
+    ws = torch.empty(max(pp.pp_op_head_bytes(h, top) for h in heads), dtype=torch.uint8, device="cuda")
+
+    def go(h, x, w, y, ids, u):
+        st = torch.cuda.current_stream().cuda_stream
+        if top:
+            pp.pp_op_head_distill(st, h, ids.data_ptr(), u.data_ptr(), top, 2.0, 0.5, y.data_ptr(), ws.data_ptr(), ws.numel())
+        else:
+            pp.pp_op_head_ce(st, h, y.data_ptr(), ws.data_ptr(), ws.numel())
+    graphs = []
+    for h, i in zip(heads, ins):
+        go(h, *i)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            go(h, *i)
+    for turn in range(3):
+        for g, i, o in zip(graphs, ins, outs):
+            g.replay()
+            torch.cuda.synchronize()
+            a = dict(ids=i[3], u=i[4], tau=2.0, share=0.5) if top else {}
+            ref = call(*i[:3], dx=grads, dw=(0, vocab) if grads else None, dw_type=torch.float32 if grads else None, **a)
+            for name, v in o.items():
+                assert np.array_equal(v.double().cpu().numpy(), ref[name]), (turn, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["ce", "mixed"])
+@pytest.mark.parametrize("n,vocab,d", [(18, 1 << 20, 8), (3, 1 << 20, 8), (20, 100, 1 << 14), (3, 100, 1 << 14), (270001, 9, 8)])
+def test_largest_sizes(n, vocab, d, kind, dtype):
+    k = dict(KINDS[kind])
+    x, w, y, ids, u = make(n, vocab, d, TYPES[dtype], top=k.pop("top"), std=0.5 if d < 64 else 0.02)
+    a = dict(ids=ids, u=u, **k) if ids is not None else {}
+    dw = (vocab - 7, vocab)
+    check(call(x, w, y, dw=dw, **a), x, w, y, dw=dw, pieces=2, **a)
+
+
 def test_refusals_name_what_is_wrong():
     x, w, y, _, _ = make(8, 100, 64, torch.bfloat16)
     h = pp.make_head(x, w, loss=torch.empty(1, device="cuda"))
