@@ -369,12 +369,12 @@ __device__ __forceinline__ void head_entries(const HeadRow& h, int t, int* id_s,
   float u = -INFINITY;
   if (j < h.top) {
     id = h.ids[(size_t)t * h.top + j];
-    if ((uint32_t)id < (uint32_t)h.V) u = h.logits[(size_t)t * h.top + j] / h.tau; else id = -1;
+    if ((uint32_t)id < (uint32_t)h.V) u = h.logits[(size_t)t * h.top + j]; else id = -1;
     if (u == -INFINITY) id = -1;
   }
   // NaN among the entries has to reach the sum: fmaxf would drop it from the maximum
   const float m = block_max(id >= 0 ? u : -INFINITY, red);
-  const float e = id >= 0 ? expf(u - m) : 0.f;
+  const float e = id >= 0 ? expf((u - m) / h.tau) : 0.f;          // the largest first: the lowest finite value over a low temperature is not finite
   const float s = block_sum(e, red);
   if (j < h.top) { id_s[j] = id; q_s[j] = id >= 0 ? e / s : 0.f; }
   __syncthreads();
@@ -712,14 +712,14 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
         const int j = lane + 64 * k;
         if (j < h.top) {
           id[k] = h.ids[(size_t)t * h.top + j];
-          if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j] * it; else id[k] = -1;
+          if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j]; else id[k] = -1;
           if (u[k] == -INFINITY) id[k] = -1;
           if (id[k] >= 0) zj[k] = zs[j];
         }
       }
       const float m = wave_max(fmaxf(id[0] >= 0 ? u[0] : -INFINITY, id[1] >= 0 ? u[1] : -INFINITY));
 #pragma unroll
-      for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf(u[k] - m) : 0.f;
+      for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf((u[k] - m) * it) : 0.f;
       const float sum = wave_sum(q[0] + q[1]), lst = logf(st);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -972,7 +972,7 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
       const int j = lane + 64 * k;
       if (j < h.top && h.share > 0.f && w != 0.f) {
         id[k] = h.ids[(size_t)t * h.top + j];
-        if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j] * it; else id[k] = -1;
+        if ((uint32_t)id[k] < (uint32_t)h.V) u[k] = h.logits[(size_t)t * h.top + j]; else id[k] = -1;
         if (u[k] == -INFINITY) id[k] = -1;
       }
     }
@@ -1015,7 +1015,7 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
       if (id[k] >= 0) zj[k] = z[id[k]];
     const float um = wave_max(fmaxf(id[0] >= 0 ? u[0] : -INFINITY, id[1] >= 0 ? u[1] : -INFINITY));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf(u[k] - um) : 0.f;
+    for (int k = 0; k < 2; ++k) q[k] = id[k] >= 0 ? expf((u[k] - um) * it) : 0.f;
     const float sum = wave_sum(q[0] + q[1]), lst = logf(s2);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {

@@ -292,6 +292,21 @@ def test_rows_wider_than_a_workgroup_holds(kind, dtype):
     assert np.isnan(bad["row_loss"][3]) and np.isnan(bad["dx"][3]).all() and not np.isnan(bad["dx"][[2, 4]]).any()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [12, 70])
+@pytest.mark.parametrize("tau,share", [(0.25, 1.0), (0.25, 0.5), (2.0, 0.5)])
+def test_entries_of_the_lowest_finite_value(tau, share, n, dtype):
+    """The lowest finite float is an entry like any other: alone in a row it has the whole probability, at any temperature."""
+    x, w, y, ids, u = make(n, 300, 64, TYPES[dtype], top=5, ragged=False)
+    low = torch.finfo(torch.float32).min
+    u[0] = low
+    u[1, 1:] = low
+    u[2, :4] = low
+    ids[3, 1:], u[3] = -1, low
+    a = dict(ids=ids, u=u, tau=tau, share=share)
+    check(call(x, w, y, dw=(0, 300), **a), x, w, y, dw=(0, 300), **a)
+
+
 def test_non_finite_rows_that_count_stay_in_their_rows():
     """NaN in a row that counts: its loss and its dX row are NaN, the other rows' are as without it."""
     x, w, y, _, _ = make(300, 500, 64, torch.bfloat16, ignored=0.0)
