@@ -84,7 +84,7 @@ HeadPlan plan_head(const HeadArgs& a) {
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
     p.rowl = take(kFew * 4);
     p.z = take((size_t)a.n * p.vp * 4);
-    p.stats = take((size_t)kFew * p.parts * 16);
+      p.stats = take((size_t)kFew * (p.parts / 4) * 16);
     p.coef = take(kFew * 16);
     p.scale = take((size_t)kFew * (a.top + 1) * 4);
     p.zsel = take((size_t)kFew * (a.top + 1) * 4);
@@ -856,7 +856,7 @@ struct HeadFew {
   const int32_t *targets, *ids;
   const float *logits, *weight;
   float tau, share;
-  float *z, *part, *coef, *sub, *psum;          // z [n][ldz], part [16][parts][4], coef [16][4], sub [16][top + 1], psum [partials][n][d]
+  float *z, *part, *coef, *sub, *psum;          // z [n][ldz], part [16][parts / 4][4], coef [16][4], sub [16][top + 1], psum [partials][n][d]
   int32_t *sid;                                 // [16][top + 1]: where sub is taken off, -1: nowhere
   float *loss, *row_loss, *row_lse;
   void *dx, *dw;
@@ -952,7 +952,16 @@ __global__ __launch_bounds__(256) void head_few_z_kernel(HeadFew h) {
   }
 #pragma unroll
   for (int o = 16; o < 64; o <<= 1) few_merge(m, s, s2, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(s2, o, 64), it);
-  if (lq == 0) *reinterpret_cast<float4*>(h.part + ((size_t)l16 * h.parts + gw) * 4) = make_float4(m, s, s2, 0.f);
+  // the workgroup's four waves, in their order
+  __shared__ float4 sum_s[4][16];
+  if (lq == 0) sum_s[threadIdx.x >> 6][l16] = make_float4(m, s, s2, 0.f);
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+  for (int k = 1; k < 4; ++k) {
+    const float4 o = sum_s[k][l16];
+    few_merge(m, s, s2, o.x, o.y, o.z, it);
+  }
+  *reinterpret_cast<float4*>(h.part + ((size_t)l16 * gridDim.x + blockIdx.x) * 4) = make_float4(m, s, s2, 0.f);
 }
 
 // One block, a wave per row: losses, and for the gradients dz = coef[1] exp(z - coef[0]) + coef[2] exp((z - coef[0]) / tau) - sub at sid (all 0 for a row that is left out)
@@ -977,25 +986,20 @@ __global__ __launch_bounds__(1024) void head_few_fin_kernel(HeadFew h) {
       }
     }
     soft = __ballot(id[0] >= 0 || id[1] >= 0) != 0;
-    // at most 2048 partial sums, 32 a lane: the maximum first, then sums that do not wait for each other; 16 loads in flight
-    const float4* part = reinterpret_cast<const float4*>(h.part) + (size_t)t * h.parts;
-    for (int k0 = lane; k0 < h.parts; k0 += 16 * 64) {
-      float v[16];
+    // at most 512 partial sums, 8 a lane: all of them requested at once, the maximum first, then sums that do not wait for each other
+    const int parts = h.parts / 4;
+    const float4* part = reinterpret_cast<const float4*>(h.part) + (size_t)t * parts;
+    constexpr int K = 2048 / 4 / 64;
+    float4 p[K];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = k0 + 64 * k < h.parts ? part[k0 + 64 * k].x : -INFINITY;
+    for (int k = 0; k < K; ++k) p[k] = lane + 64 * k < parts ? part[lane + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int k = 0; k < 16; ++k) m = fmaxf(m, v[k]);
-    }
+    for (int k = 0; k < K; ++k) m = fmaxf(m, p[k].x);
     m = wave_max(m);
-    for (int k0 = lane; k0 < h.parts; k0 += 16 * 64) {
-      float4 p[16];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) p[k] = k0 + 64 * k < h.parts ? part[k0 + 64 * k] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        s += p[k].x == -INFINITY ? p[k].y : p[k].y * expf(p[k].x - m);          // a part without a finite logit has a sum of 0, or NaN
-        if (it != 1.f) s2 += p[k].x == -INFINITY ? p[k].z : p[k].z * expf((p[k].x - m) * it);
-      }
+    for (int k = 0; k < K; ++k) {
+      s += p[k].x == -INFINITY ? p[k].y : p[k].y * expf(p[k].x - m);          // a part without a finite logit has a sum of 0, or NaN
+      if (it != 1.f) s2 += p[k].x == -INFINITY ? p[k].z : p[k].z * expf((p[k].x - m) * it);
     }
     s = wave_sum(s);
     s2 = it == 1.f ? s : wave_sum(s2);
