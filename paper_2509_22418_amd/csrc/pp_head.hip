@@ -61,6 +61,8 @@ int capped(int splits, double mn, size_t cap) {
 
 // Few rows: threads of a workgroup side by side (8 columns each), and rows of W per workgroup such that the workgroups' partial sums of dX are kFewPartials at most.
 constexpr int kFew = 16, kFewPartials = 512;
+// Small vocabularies of long rows: the four waves of a workgroup take a quarter of 16 rows of W each (2 rows of X, 5280 x 3999 in fp32: 70 -> 45 us)
+bool few_split(int tiles, int d) { return tiles <= 512 && d > 256; }
 int few_cols(int d) { int c = 1; while (c < 256 && c * 8 < d) c *= 2; return c; }
 int few_chunk(int rows, int d) { return std::max((rows + kFewPartials - 1) / kFewPartials, 2 * 256 / few_cols(d)); }          // two rows for every thread at least
 
@@ -79,6 +81,7 @@ HeadPlan plan_head(const HeadArgs& a) {
     // up to 2048 waves, 8 a compute unit, each with as many of the blocks of 16 rows of W as any other
     const int tiles = (a.vocab + 15) / 16, each = (tiles + 2047) / 2048;
     p.parts = ((tiles + each - 1) / each + 3) / 4 * 4;
+    if (few_split(tiles, a.d)) p.parts = 4 * tiles;
     p.vp = pad_to(a.vocab, 16);
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += (bytes + 255) / 256 * 256; return o; };
@@ -908,33 +911,43 @@ __device__ __forceinline__ void few_merge(float& m, float& s, float& s2, float m
   m = top;
 }
 
-template <class T>
+template <class T, bool SPLIT>          // SPLIT: a quarter of 16 rows of W for each of a workgroup's waves
 __global__ __launch_bounds__(256) void head_few_z_kernel(HeadFew h) {
   constexpr int E = FewChunk<T>::E, U = 8, STEP = 4 * E;          // k per MFMA step of the four lane groups
   const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4, gw = blockIdx.x * 4 + (threadIdx.x >> 6);
   const T* x = (const T*)h.x + (size_t)min(l16, h.n - 1) * h.ldx;
   const float it = 1.0f / h.tau;
   float m = -INFINITY, s = 0.f, s2 = 0.f;
-  for (int tile = gw; tile * 16 < h.V; tile += h.parts) {
+  [[maybe_unused]] __shared__ few_f32x4 acc_s[4][64];
+  const int wave = threadIdx.x >> 6, quarter = SPLIT ? (h.d + 4 * STEP - 1) / (4 * STEP) * STEP : h.d;
+  const int kb = SPLIT ? wave * quarter : 0, ke = min(kb + quarter, h.d);
+  for (int tile = SPLIT ? blockIdx.x : gw; tile * 16 < h.V; tile += SPLIT ? gridDim.x : h.parts) {
     const T* w = (const T*)h.w + (size_t)min(tile * 16 + l16, h.V - 1) * h.ldw;
     few_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     uint4 a[2][U], b[2][U];
     auto fetch = [&](int buf, int k0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) a[buf][u] = few_load<T>(w, k0 + u * STEP + lq * E, h.d);
+      for (int u = 0; u < U; ++u) a[buf][u] = few_load<T>(w, k0 + u * STEP + lq * E, ke);
 #pragma unroll
-      for (int u = 0; u < U; ++u) b[buf][u] = few_load<T>(x, k0 + u * STEP + lq * E, h.d);
+      for (int u = 0; u < U; ++u) b[buf][u] = few_load<T>(x, k0 + u * STEP + lq * E, ke);
     };
     auto multiply = [&](int buf) {
 #pragma unroll
       for (int u = 0; u < U; ++u) few_mfma(acc, a[buf][u], b[buf][u], T{});
     };
-    fetch(0, 0);
-    for (int k0 = 0; k0 < h.d; k0 += 2 * U * STEP) {          // chunks behind d are zeros without a load
+    fetch(0, kb);
+    for (int k0 = kb; k0 < ke; k0 += 2 * U * STEP) {          // chunks behind the last are zeros without a load
       fetch(1, k0 + U * STEP);
       multiply(0);
       fetch(0, k0 + 2 * U * STEP);
       multiply(1);
+    }
+    if constexpr (SPLIT) {          // the quarters in their order; the first wave goes on with the sum
+      acc_s[wave][lane] = acc;
+      __syncthreads();
+      acc = acc_s[0][lane] + acc_s[1][lane] + acc_s[2][lane] + acc_s[3][lane];
+      __syncthreads();
+      if (wave) continue;
     }
     // element r: row 4 lq + r of the 16 rows of W, token l16
     const int v0 = tile * 16 + 4 * lq;
@@ -1307,7 +1320,8 @@ template <class T>
 static void head_few(hipStream_t st, const HeadArgs& a, const HeadPlan& p, char* ws, float* row_loss) {
   HeadFew h{a.x, a.w, a.ldx, a.ldw, a.n, a.vocab, a.d, p.vp, p.parts, a.top, a.dw_lo, a.dw_hi, a.lddx, a.lddw, a.dw_f32 == 2, 0, 0, a.targets, a.ids, a.logits, a.row_weight, a.tau, a.share,
             (float*)(ws + p.z), (float*)(ws + p.stats), (float*)(ws + p.coef), (float*)(ws + p.scale), (float*)(ws + p.part), (int32_t*)(ws + p.zsel), a.loss, row_loss, a.row_lse, a.dx, a.dw};
-  head_few_z_kernel<T><<<p.parts / 4, 256, 0, st>>>(h);
+  if (few_split((a.vocab + 15) / 16, a.d)) head_few_z_kernel<T, true><<<p.parts / 4, 256, 0, st>>>(h);
+  else head_few_z_kernel<T, false><<<p.parts / 4, 256, 0, st>>>(h);
   head_few_fin_kernel<<<1, 1024, 0, st>>>(h);
   if (!a.dx && !a.dw) return;
   if (a.n == 1) few_grads<T, 1>(st, a, h);
