@@ -64,7 +64,13 @@ constexpr int kFew = 16, kFewPartials = 512;
 // Small vocabularies of long rows: the four waves of a workgroup take a quarter of 16 rows of W each (2 rows of X, 5280 x 3999 in fp32: 70 -> 45 us)
 bool few_split(int tiles, int d) { return tiles <= 512 && d > 256; }
 int few_cols(int d) { int c = 1; while (c < 256 && c * 8 < d) c *= 2; return c; }
-int few_chunk(int rows, int d) { return std::max((rows + kFewPartials - 1) / kFewPartials, 2 * 256 / few_cols(d)); }          // two rows for every thread at least
+int few_waves(int d) { return d > 256 ? 4 : d > 128 ? 2 : 1; }          // waves side by side where dX is formed by MFMAs, 128 columns each
+// rows of W per workgroup of dX: one row of X (vector units) two for every thread at least; more rows (MFMAs) as many as make 1024 workgroups with the column slices
+int few_chunk(int rows, int d, int n) {
+  if (n == 1) return std::max((rows + kFewPartials - 1) / kFewPartials, 2 * 256 / few_cols(d));
+  const int slice = few_waves(d) * 128, groups = std::max(1, std::min(kFewPartials, 1024 / ((d + slice - 1) / slice)));
+  return std::max((rows + groups - 1) / groups, 32);
+}
 
 HeadPlan plan_head(const HeadArgs& a) {
   HeadPlan p{};
@@ -92,7 +98,7 @@ HeadPlan plan_head(const HeadArgs& a) {
     p.scale = take((size_t)kFew * (a.top + 1) * 4);
     p.zsel = take((size_t)kFew * (a.top + 1) * 4);
     if (a.dx) {
-      const int chunk = few_chunk(a.vocab, a.d);
+      const int chunk = few_chunk(a.vocab, a.d, a.n);
       p.part = take((size_t)((a.vocab + chunk - 1) / chunk) * a.n * a.d * 4);
     }
     p.total = off;
@@ -1099,31 +1105,18 @@ __device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float
   }
   __syncthreads();
 }
-template <int NT> __device__ __forceinline__ void few_row(const float* dz, float g[NT]) {          // four tokens a read
-  if constexpr (NT % 4 == 0) {
-#pragma unroll
-    for (int t = 0; t < NT; t += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(dz + t);
-      g[t] = v.x; g[t + 1] = v.y; g[t + 2] = v.z; g[t + 3] = v.w;
-    }
-  } else
-#pragma unroll
-    for (int t = 0; t < NT; ++t) g[t] = dz[t];
-}
 // Threads of a workgroup: `cols` of them side by side, 8 columns each, 256 / cols rows of W at a time
-template <class T, int NT>
-__device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[NT], float (*red)[1024]) {
+template <class T>
+__device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[1], float* red) {          // one row of X
   const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
   const int lo = blockIdx.x * h.chunk, hi = min(lo + h.chunk, h.V);
-  float acc[NT][8];
+  float acc[8];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[t][e] = 0.f;
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   const T* w = (const T*)h.w;
   for (int v0 = lo; v0 < hi; v0 += 128) {
     const int rows = min(128, hi - v0);
-    few_dz<NT>(h, v0, rows, dz);
+    few_dz<1>(h, v0, rows, dz);
     if (c >= h.d) continue;          // uniform barriers: few_dz is reached by every thread at every trip
     auto row = [&](int r) {
       float v[8];
@@ -1132,12 +1125,9 @@ __device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[N
       else
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < h.d ? to_f32(p[e]) : 0.f;
-      float g[NT];
-      few_row<NT>(dz[r], g);
+      const float g = dz[r][0];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[t][e] = fmaf(g[t], v[e], acc[t][e]);
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(g, v[e], acc[e]);
     };
     int r = rg;
     for (; r + 3 * rp < rows; r += 4 * rp) { row(r); row(r + rp); row(r + 2 * rp); row(r + 3 * rp); }
@@ -1146,33 +1136,26 @@ __device__ __forceinline__ void few_dx(const HeadFew& h, int cols, float (*dz)[N
   // The workgroup's sums of a column: lanes of a wave, then waves one after the other by way of shared memory, the last one stores
   for (int o = cols; o < 64; o <<= 1)
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[t][e] += __shfl_xor(acc[t][e], o, 64);
-  constexpr int HT = NT < 8 ? NT : 8;          // tokens at a time
-  const int wave = threadIdx.x >> 6, rows_at = cols <= 64 ? wave : rg, last = cols <= 64 ? 3 : rp - 1;
+    for (int e = 0; e < 8; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  const int rows_at = cols <= 64 ? threadIdx.x >> 6 : rg, last = cols <= 64 ? 3 : rp - 1;
   const bool holds = cols >= 64 || (threadIdx.x & 63) < cols;
-  float* out = h.psum + (size_t)blockIdx.x * h.n * h.d;
+  float* out = h.psum + (size_t)blockIdx.x * h.d;
+  for (int k = 0; k <= last; ++k) {
+    if (rows_at == k && holds) {
+      float* at = red + ((cg * 8) & 1023);          // cols 256: one row at a time, nothing to add
+      if (k > 0)
 #pragma unroll
-  for (int t0 = 0; t0 < NT; t0 += HT)
-    for (int w = 0; w <= last; ++w) {
-      if (rows_at == w && holds)
+        for (int e = 0; e < 8; ++e) acc[e] += at[e];
+      if (k < last)
 #pragma unroll
-        for (int t = 0; t < HT; ++t) {
-          float* at = &red[t][(cg * 8) & 1023];          // cols 256: one row at a time, nothing to add
-          if (w > 0)
+        for (int e = 0; e < 8; ++e) at[e] = acc[e];
+      else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[t0 + t][e] += at[e];
-          if (w < last)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) at[e] = acc[t0 + t][e];
-          else if (t0 + t < h.n)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (c + e < h.d) out[(size_t)(t0 + t) * h.d + c + e] = acc[t0 + t][e];
-        }
-      __syncthreads();
+        for (int e = 0; e < 8; ++e)
+          if (c + e < h.d) out[c + e] = acc[e];
     }
+    __syncthreads();
+  }
 }
 // dx = sum of the partials, a block per row and 64 columns, 16 waves of partials
 template <class T>
@@ -1194,27 +1177,22 @@ __global__ __launch_bounds__(1024) void head_few_sum_kernel(HeadFew h, int parti
   for (int k = 1; k < 16; ++k) s += s_s[k][lane];
   ((T*)h.dx)[(size_t)t * h.lddx + c] = from_f32<T>(h.coef[t * 4 + 3] != 0.f ? s : 0.f);
 }
-template <class T, class TO, int NT>
-__device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, float (*dz)[NT]) {
+template <class T, class TO>
+__device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, float (*dz)[1]) {          // one row of X
   const int rp = 256 / cols, cg = threadIdx.x % cols, rg = threadIdx.x / cols, c = (blockIdx.y * cols + cg) * 8;
   const int lo = h.dw_lo + group * h.chunk_dw, hi = min(lo + h.chunk_dw, h.dw_hi);
-  float x[NT][8];
+  float x[8];
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[t][e] = t < h.n && c + e < h.d && h.coef[t * 4 + 3] != 0.f ? to_f32(((const T*)h.x)[(size_t)t * h.ldx + c + e]) : 0.f;
+  for (int e = 0; e < 8; ++e) x[e] = c + e < h.d && h.coef[3] != 0.f ? to_f32(((const T*)h.x)[c + e]) : 0.f;
   for (int v0 = lo; v0 < hi; v0 += 128) {
     const int rows = min(128, hi - v0);
-    few_dz<NT>(h, v0, rows, dz);
+    few_dz<1>(h, v0, rows, dz);
     if (c >= h.d) continue;
     for (int r = rg; r < rows; r += rp) {
-      float o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      float g[NT];
-      few_row<NT>(dz[r], g);
+      const float g = dz[r][0];
+      float o[8];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = fmaf(g[t], x[t][e], o[e]);
+      for (int e = 0; e < 8; ++e) o[e] = g * x[e];
       TO* p = (TO*)h.dw + (size_t)(v0 + r - h.dw_lo) * h.lddw + c;
       const bool whole = c + 8 <= h.d && h.lddw % 8 == 0 && ((uintptr_t)h.dw & 15) == 0;
       if (h.dw_add)
@@ -1228,13 +1206,127 @@ __device__ __forceinline__ void few_dw(const HeadFew& h, int cols, int group, fl
   }
 }
 
+// dX of several rows by fp32 MFMAs: four rows of W at a time are the second operand, a lane's eight columns eight instructions apart, dz of those rows the first.  16 tokens cost the vector units
+// 128 multiply-adds for 16 bytes of W, more than the memory takes to deliver them (dX and dW of 16 x 768 x 32000 115 -> 77 us, 8 x 512 x 5000 47 -> 23).
+template <class T, int NT>
+__device__ __forceinline__ void few_dx_mfma(const HeadFew& h, int waves, float (*dz)[NT], float (*red)[256]) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4, wave = threadIdx.x >> 6;
+  const int wcol = wave % waves, wrow = wave / waves, rows_at = 4 * (4 / waves), c0 = (blockIdx.y * waves + wcol) * 128, c = c0 + l16 * 8;
+  const int lo = blockIdx.x * h.chunk, hi = min(lo + h.chunk, h.V);
+  few_f32x4 acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = few_f32x4{0.f, 0.f, 0.f, 0.f};
+  constexpr int U = 4;
+  for (int v0 = lo; v0 < hi; v0 += 128) {
+    const int rows = min(128, hi - v0);
+    few_dz<NT>(h, v0, rows, dz);
+    if (c0 >= h.d) continue;          // uniform barriers: few_dz is reached by every thread at every trip
+    for (int r = 4 * wrow; r < rows; r += U * rows_at) {
+      float w[U][8], a[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int rr = r + u * rows_at + lq;
+        const T* p = (const T*)h.w + (size_t)(v0 + min(rr, rows - 1)) * h.ldw + c;
+        if (c + 8 <= h.d) few_load8(p, w[u]);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[u][e] = c + e < h.d ? to_f32(p[e]) : 0.f;
+        a[u] = rr < rows && l16 < NT ? dz[rr][l16 & (NT - 1)] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u], w[u][e], acc[e], 0, 0, 0);
+    }
+  }
+  // element r of acc[e]: token 4 lq + r, column c + e.  Waves of the same columns one after the other by way of shared memory, the last one stores.
+  float* out = h.psum + (size_t)blockIdx.x * h.n * h.d;
+  const int last = 4 / waves - 1;
+  for (int k = 0; k <= last; ++k) {
+    if (wrow == k)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float* at = &red[4 * lq + r][(wcol * 128 + l16 * 8) & 255];          // four waves side by side: nothing to add
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = acc[e][r] + (k > 0 ? at[e] : 0.f);
+        if (k < last) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) at[e] = v[e];
+        } else if (4 * lq + r < h.n) {
+          float* o = out + (size_t)(4 * lq + r) * h.d;
+          store_cols(o, c, h.d, make_float4(v[0], v[1], v[2], v[3]));
+          store_cols(o, c + 4, h.d, make_float4(v[4], v[5], v[6], v[7]));
+        }
+      }
+    __syncthreads();
+  }
+}
+
+// dW of several rows likewise: 16 rows of W at a time, dz of four tokens the first operand, their rows of X (held by the lanes) the second
+template <class T, class TO, int NT>
+__device__ __forceinline__ void few_dw_mfma(const HeadFew& h, int waves, int group, float (*dz)[NT]) {
+  const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4, wave = threadIdx.x >> 6;
+  const int wcol = wave % waves, wrow = wave / waves, c0 = (blockIdx.y * waves + wcol) * 128, c = c0 + l16 * 8;
+  const int lo = h.dw_lo + group * h.chunk_dw, hi = min(lo + h.chunk_dw, h.dw_hi);
+  float x[NT / 4][8];
+#pragma unroll
+  for (int s = 0; s < NT / 4; ++s) {
+    const int t = 4 * s + lq;
+    const bool there = t < h.n && h.coef[t * 4 + 3] != 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[s][e] = there && c + e < h.d ? to_f32(((const T*)h.x)[(size_t)t * h.ldx + c + e]) : 0.f;
+  }
+  for (int v0 = lo; v0 < hi; v0 += 128) {
+    const int rows = min(128, hi - v0);
+    few_dz<NT>(h, v0, rows, dz);
+    if (c0 >= h.d) continue;
+    for (int r0 = 16 * wrow; r0 < rows; r0 += 16 * (4 / waves)) {
+      few_f32x4 acc[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = few_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < NT / 4; ++s) {
+        const float a = r0 + l16 < rows ? dz[r0 + l16][4 * s + lq] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, x[s][e], acc[e], 0, 0, 0);
+      }
+      // element r of acc[e]: row 4 lq + r, column c + e
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = r0 + 4 * lq + r;
+        if (row >= rows) continue;
+        TO* p = (TO*)h.dw + (size_t)(v0 + row - h.dw_lo) * h.lddw;
+        float4 o0 = make_float4(acc[0][r], acc[1][r], acc[2][r], acc[3][r]), o1 = make_float4(acc[4][r], acc[5][r], acc[6][r], acc[7][r]);
+        if constexpr (sizeof(TO) == 4)
+          if (h.dw_add) {
+            const float4 b0 = load_cols((const float*)p, c, h.d), b1 = load_cols((const float*)p, c + 4, h.d);
+            o0.x += b0.x; o0.y += b0.y; o0.z += b0.z; o0.w += b0.w;
+            o1.x += b1.x; o1.y += b1.y; o1.z += b1.z; o1.w += b1.w;
+          }
+        if (sizeof(TO) == 2 && c + 8 <= h.d)
+          *reinterpret_cast<any16*>(p + c) = any16{{f32x2_to_bf16x2(o0.x, o0.y), f32x2_to_bf16x2(o0.z, o0.w), f32x2_to_bf16x2(o1.x, o1.y), f32x2_to_bf16x2(o1.z, o1.w)}};
+        else {
+          store_cols(p, c, h.d, o0);
+          store_cols(p, c + 4, h.d, o1);
+        }
+      }
+    }
+  }
+}
+
 // The first `groups` workgroups form dX's partial sums, the others dW: neither waits for the other, so they share a launch (8 x 512 x 5000 60.6 -> 55.4 us, one row of 2048 x 32000 90 -> 81)
 template <class T, class TO, int NT>
-__global__ __launch_bounds__(256) void head_few_grads_kernel(HeadFew h, int cols, int groups) {
+__global__ __launch_bounds__(256) void head_few_grads_kernel(HeadFew h, int cols, int waves, int groups) {
   __shared__ __align__(16) float dz[128][NT];
-  __shared__ float red[NT < 8 ? NT : 8][1024];
-  if ((int)blockIdx.x < groups) few_dx<T, NT>(h, cols, dz, red);
-  else few_dw<T, TO, NT>(h, cols, blockIdx.x - groups, dz);
+  __shared__ float red[NT == 1 ? 1024 : 16 * 256];
+  if ((int)blockIdx.x < groups) {
+    if constexpr (NT == 1) few_dx<T>(h, cols, dz, red);
+    else few_dx_mfma<T, NT>(h, waves, dz, reinterpret_cast<float(*)[256]>(red));
+  } else if constexpr (NT == 1)
+    few_dw<T, TO>(h, cols, blockIdx.x - groups, dz);
+  else
+    few_dw_mfma<T, TO, NT>(h, waves, blockIdx.x - groups, dz);
 }
 
 // ------------------------------------------------------------------------------------------------ outputs
@@ -1307,13 +1399,15 @@ static dim3 quads(int rows) { return dim3((rows + 3) / 4); }
 
 template <class T, int NT>
 static void few_grads(hipStream_t st, const HeadArgs& a, HeadFew h) {
-  const int cols = few_cols(a.d), slices = (a.d + cols * 8 - 1) / (cols * 8), rows = a.dw ? a.dw_hi - a.dw_lo : 0;
-  h.chunk = few_chunk(a.vocab, a.d);
-  h.chunk_dw = std::max(1, std::min(128, (rows * slices + 1023) / 1024));
+  const int cols = few_cols(a.d), waves = few_waves(a.d), rows = a.dw ? a.dw_hi - a.dw_lo : 0;
+  const int slice = NT == 1 ? cols * 8 : waves * 128, slices = (a.d + slice - 1) / slice;
+  h.chunk = few_chunk(a.vocab, a.d, a.n);
+  h.chunk_dw = std::max(1, std::min(128, (int)(((long)rows * slices + 1023) / 1024)));
+  if (NT > 1) h.chunk_dw = (h.chunk_dw + 15) / 16 * 16;
   const int groups = a.dx ? (a.vocab + h.chunk - 1) / h.chunk : 0;
   const dim3 grid(groups + (rows + h.chunk_dw - 1) / h.chunk_dw, slices);
-  if (a.dw_f32) head_few_grads_kernel<T, float, NT><<<grid, 256, 0, st>>>(h, cols, groups);
-  else head_few_grads_kernel<T, T, NT><<<grid, 256, 0, st>>>(h, cols, groups);
+  if (a.dw_f32) head_few_grads_kernel<T, float, NT><<<grid, 256, 0, st>>>(h, cols, waves, groups);
+  else head_few_grads_kernel<T, T, NT><<<grid, 256, 0, st>>>(h, cols, waves, groups);
   if (a.dx) head_few_sum_kernel<T><<<dim3((a.d + 63) / 64, a.n), 1024, 0, st>>>(h, groups);
 }
 template <class T>
