@@ -1088,15 +1088,23 @@ __device__ __forceinline__ void few_dz(const HeadFew& h, int v0, int rows, float
   const float it = 1.0f / h.tau;
   __syncthreads();
   const int lg = 32 - __clz(max(rows - 1, 1)), all = NT << lg;          // 2 ^ lg >= rows
-  for (int i = threadIdx.x; i < all; i += 256) {
-    const int t = i >> lg, r = i & ((1 << lg) - 1);
-    float v = 0.f;
-    if (t < h.n && r < rows) {
-      const float4 c = *reinterpret_cast<const float4*>(h.coef + t * 4);
-      const float a = h.z[(size_t)t * h.ldz + v0 + r] - c.x;
-      if (c.w != 0.f) v = (c.y != 0.f ? c.y * expf(a) : 0.f) + (c.z != 0.f ? c.z * expf(a * it) : 0.f);
+  constexpr int K = NT < 8 ? 1 : NT / 4;          // elements of a thread at a time, their loads in flight together
+  for (int i0 = threadIdx.x; i0 < all; i0 += 256 * K) {
+    float4 c[K];
+    float z[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = i0 + 256 * k, t = min(i >> lg, h.n - 1), r = min(i & ((1 << lg) - 1), rows - 1);
+      c[k] = *reinterpret_cast<const float4*>(h.coef + t * 4);
+      z[k] = h.z[(size_t)t * h.ldz + v0 + r];
     }
-    dz[r][t] = v;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int i = i0 + 256 * k, t = i >> lg, r = i & ((1 << lg) - 1);
+      if (i >= all) break;
+      const float a = z[k] - c[k].x;
+      dz[r][t] = t < h.n && r < rows && c[k].w != 0.f ? (c[k].y != 0.f ? c[k].y * expf(a) : 0.f) + (c[k].z != 0.f ? c[k].z * expf(a * it) : 0.f) : 0.f;
+    }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < h.n * (h.top + 1); i += 256) {          // no two entries of a row have the same place
