@@ -64,7 +64,7 @@ constexpr int kFew = 16, kFewPartials = 512;
 // Small vocabularies of long rows: the four waves of a workgroup take a quarter of 16 rows of W each (2 rows of X, 5280 x 3999 in fp32: 70 -> 45 us)
 bool few_split(int tiles, int d) { return tiles <= 512 && d > 256; }
 int few_cols(int d) { int c = 1; while (c < 256 && c * 8 < d) c *= 2; return c; }
-int few_waves(int d) { return d > 256 ? 4 : d > 128 ? 2 : 1; }          // waves side by side where dX is formed by MFMAs, 128 columns each
+int few_waves(int d) { return d > 256 ? 4 : d > 128 ? 2 : 1; }          // waves side by side where dX and dW are formed by MFMAs, 128 columns each (from two rows on: 4 x 2048 x 32000 dX 74 -> 71 us, 16 x 768 69 -> 56; one row has too little to multiply)
 // rows of W per workgroup of dX: one row of X (vector units) two for every thread at least; more rows (MFMAs) as many as make 1024 workgroups with the column slices
 int few_chunk(int rows, int d, int n) {
   if (n == 1) return std::max((rows + kFewPartials - 1) / kFewPartials, 2 * 256 / few_cols(d));
