@@ -10,7 +10,7 @@
 // is relative.  With s = sum e the row of dz is a multiple of e but for the target and the entries:
 //     dz = C (e - sub / C),  C = g c / s,  sub = g (c1 [v = y] + ct Q):
 // a kernel over rows replaces e at those few places, and C is applied to dX's rows behind their product and to X's rows in front of dW's.  No other pass over the piece, and no second
-// product of logits: 2 products for dX alone, 3 with dW.  Rows whose largest logit turns out to lie more than kFar above the reference take the maximum, and the first product of
+// product of logits: 2 products for dX alone, 3 with dW.  Rows whose largest logit turns out to lie more than kFar from the reference take the maximum, and the first product of
 // their 256-row blocks is done again (by a launch that ends at once where there are none).  Two softmaxes at once (tau != 1 beside hard targets) take one more pass
 // over the piece, which forms both exponentials from the one exponent that the first product then stores.
 // Pieces are of rows, not of the vocabulary: a piece of vocabulary would have to wait for the sums of all others, hence form its logits twice (4 products instead of 3), and sum dX in
@@ -519,16 +519,20 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
   bf16_t* xc = h.xc + (size_t)i * h.dp;
   float* zs = h.zsel + (size_t)i * (h.top + 1);
   float best = -INFINITY;
-  // Entries in groups over blockIdx.y (the first entry alone, group 1, where the first product picks all logits), the target (entry `top`) and the row's copy with the first; the reference is the largest of that first group.
+  // Entries in groups over blockIdx.y (the first entry alone, group 1, where the first product picks all logits), the target (entry `top`) and the row's copy with the first; the reference is the largest of that first group,
+  // or the row's first entry where the group has none and the row no target: a reference far above all logits would lose every exponential.
   constexpr int NB = 8;          // entries at a time: eight rows of W in flight
   int lo = blockIdx.y * h.group, hi = soft ? min(lo + h.group, h.top) : lo;
-  if (h.group == 1 && soft) {          // the first entry there is
-    uint64_t there = 0;
-    for (int j = 0; j < h.top && !there; j += 64) {
+  auto first_entry = [&]() {          // the first entry there is, -1 if none is
+    for (int j = 0; j < h.top; j += 64) {
       const bool is = j + lane < h.top && (uint32_t)h.ids[(size_t)t * h.top + j + lane] < (uint32_t)h.V && h.logits[(size_t)t * h.top + j + lane] != -INFINITY;
-      there = __ballot(is);
-      if (there) { lo = j + __ffsll((unsigned long long)there) - 1; hi = lo + 1; }
+      if (const uint64_t there = __ballot(is)) return j + (int)__ffsll((unsigned long long)there) - 1;
     }
+    return -1;
+  };
+  if (h.group == 1 && soft) {
+    const int j = first_entry();
+    if (j >= 0) { lo = j; hi = j + 1; }
   }
   if (blockIdx.y && lo >= hi) return;
   const int list = hi - lo + (blockIdx.y == 0);          // entries of this wave, the target last
@@ -537,9 +541,9 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
     float s[NB];
 #pragma unroll
     for (int e = 0; e < NB; ++e) {
-      const int j = lo + k0 + e;
-      id[e] = j < hi ? h.ids[(size_t)t * h.top + j] : j == hi && blockIdx.y == 0 && hard ? h.targets[t] : -1;
-      if ((uint32_t)id[e] >= (uint32_t)h.V || (j < hi && h.logits[(size_t)t * h.top + j] == -INFINITY)) id[e] = -1;
+      const int j = lo + k0 + e, v = j < hi ? h.ids[(size_t)t * h.top + j] : j == hi && blockIdx.y == 0 && hard ? h.targets[t] : -1;
+      const float uj = j < hi ? h.logits[(size_t)t * h.top + j] : 0.f;
+      id[e] = (uint32_t)v < (uint32_t)h.V && uj != -INFINITY ? v : -1;
       s[e] = 0.f;
     }
     const bool copy = blockIdx.y == 0 && k0 == 0;
@@ -573,7 +577,23 @@ __global__ __launch_bounds__(256) void head_ref_kernel(HeadRef h) {
         best = fmaxf(best, z);
       }
   }
-  if (lane == 0 && blockIdx.y == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
+  if (blockIdx.y) return;
+  if (soft && best == -INFINITY) {          // no target, and nothing in the first group: the first entry there is, whose dot product another wave forms too
+    const int j = first_entry();
+    float s = 0.f;
+    if (j >= 0) {
+      const bf16_t* w = h.w + (size_t)h.ids[(size_t)t * h.top + j] * h.ldw;
+      for (int c = lane * 8; c < h.dp; c += 512) {
+        float xv[8], wv[8];
+        load8(xc + c, xv);          // this lane's own stores
+        load8(w + c, wv);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s = fmaf(xv[k], wv[k], s);
+      }
+      best = wave_sum(s);
+    }
+  }
+  if (lane == 0) h.ref[i] = fabsf(best) < INFINITY ? best : 0.f;
 }
 
 // The entries of 128 compact rows sorted by groups of 64 columns, for the first product to pick their logits from its accumulators (HeadEpi's offs and list).  The order within a group
@@ -699,7 +719,7 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
     // Largest exponent, of the sharper one of two softmaxes, as a power of two.  Such a row takes its maximum as reference (what the rest of this
     // kernel makes of it is overwritten when its block is done again).
     const float span = far * 0.693147181f;
-    if (!OWN && !h.again && span > kFar && far < 1e30f && lane == 0) {
+    if (!OWN && !h.again && fabsf(span) > kFar && fabsf(far) < 1e30f && lane == 0) {          // (below -kFar: the reference was 0, those logits not being finite)
       h.ref[h.i0 + b0 + r] += span * (h.mixed ? fminf(1.f, h.tau) : h.tau);
       h.redo[0] = 1;
       h.redo[1 + b0 / 256] = 1;

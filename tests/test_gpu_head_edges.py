@@ -1,0 +1,37 @@
+"""Losses of the output head where their references, weights and 16-bit exponents are under strain: every output finite and within bounds that follow the roundings one by one."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_head import TYPES, call, check, make
+
+pytestmark = pytest.mark.gpu
+
+
+def strict(got, *a, **k):
+    """check(), and no output is NaN or infinite (its bounds on dx and dw are comparisons, which NaN passes)."""
+    for name, v in got.items():
+        assert np.isfinite(v).all(), (name, int((~np.isfinite(v)).sum()), np.argwhere(~np.isfinite(v))[:3].tolist())
+    return check(got, *a, **k)
+
+
+# n, vocab, entries, absent ones in front: bf16, a group of entries per wave is 4 (40 and 900 rows) or 16 (600); 900 x 8200: losses alone go by the reference too
+@pytest.mark.parametrize("n,vocab,top,gone,dtype", [(40, 600, 24, 6, "bf16"), (600, 5000, 40, 16, "bf16"), (600, 5000, 40, 35, "bf16"), (900, 8200, 6, 4, "bf16"), (40, 600, 24, 6, "f32"),
+                                                    (12, 600, 24, 6, "bf16"), (3, 600, 128, 70, "f32")])
+@pytest.mark.parametrize("tau,share", [(1.0, 1.0), (0.25, 1.0), (2.0, 0.5), (0.25, 0.5), (1.0, 0.5)])
+@pytest.mark.parametrize("by", ["id", "logit"])
+def test_rows_whose_first_entries_are_absent(n, vocab, top, gone, dtype, tau, share, by):
+    """The first entries of a row are none, it has no target, and all its logits lie far below 0 (or above): the softmax has the same weights wherever the entries stand in the list."""
+    print(f"case head late entries {n}x{vocab} top={top} gone={gone} by={by} {dtype} tau={tau} share={share}", flush=True)
+    x, w, y, ids, u = make(n, vocab, 64, TYPES[dtype], top=top, ragged=False, seed=7)
+    if by == "id":
+        ids[:, :gone:2], ids[:, 1:gone:2], u[:, :gone] = -1, vocab, torch.nan
+    else:
+        u[:, :gone] = -torch.inf
+    y[::2] = -1
+    w[:, 0] = 1.0
+    low = -100.0 * min(1.0, tau)
+    x[:, 0] = torch.tensor([low, 0.0, low / 3, low, -low, 3 * low], device="cuda").repeat(n)[:n]
+    a = dict(ids=ids, u=u, tau=tau, share=share)
+    strict(call(x, w, y, dw=(0, vocab), **a), x, w, y, dw=(0, vocab), **a)
+    strict(call(x, w, y, dx=False, **a), x, w, y, **a)
