@@ -8,8 +8,8 @@
 // bf16: the first product's epilogue stores e = exp((z - r) / tau) instead of z, r a reference of the row that is known BEFORE the product: the largest logit among the target's and
 // the teacher's entries.  A softmax needs no more of its reference than that no exponential overflows or is lost, so the maximum itself is not waited for, and e's rounding to bf16
 // is relative.  With s = sum e the row of dz is a multiple of e but for the target and the entries:
-//     dz = C (e - sub / C),  C = g c / s,  sub = g (c1 [v = y] + ct Q):
-// a kernel over rows replaces e at those few places, and C is applied to dX's rows behind their product and to X's rows in front of dW's.  No other pass over the piece, and no second
+//     dz = g C (e - sub / C),  C = c / s,  sub = c1 [v = y] + ct Q,  g the row's weight:
+// a kernel over rows replaces e at those few places, and g C is applied to dX's rows behind their product and to X's rows in front of dW's.  No other pass over the piece, and no second
 // product of logits: 2 products for dX alone, 3 with dW.  Rows whose largest logit turns out to lie more than kFar from the reference take the maximum, and the first product of
 // their 256-row blocks is done again (by a launch that ends at once where there are none).  Two softmaxes at once (tau != 1 beside hard targets) take one more pass
 // over the piece, which forms both exponentials from the one exponent that the first product then stores.
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(1024) void head_lists_kernel(const int32_t* __restr
   each([&](int r, int j, int id) { l[atomicAdd(&cnt[id >> 6], 1)] = r | (id & 63) << 7 | j << 13; });
 }
 
-// A block per 16 compact rows of the piece: sums over the column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale C, and the new values of e at the target and the
+// A block per 16 compact rows of the piece: sums over the column groups in a fixed order, then a wave per row: loss, log-sum-exp, scale g C, and the new values of e at the target and the
 // entries.  `again`: only rows of blocks that were done again.
 struct HeadFin {
   const float2* stats;
@@ -717,14 +717,16 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
     }
     const float sa = wave_sum(sl), st = h.mixed ? wave_sum(sl2) : sa;          // of the hard targets' softmax and of the teacher's (one and the same unless mixed)
     // Largest exponent, of the sharper one of two softmaxes, as a power of two.  Such a row takes its maximum as reference (what the rest of this
-    // kernel makes of it is overwritten when its block is done again).
-    const float span = far * 0.693147181f;
-    if (!OWN && !h.again && fabsf(span) > kFar && fabsf(far) < 1e30f && lane == 0) {          // (below -kFar: the reference was 0, those logits not being finite)
-      h.ref[h.i0 + b0 + r] += span * (h.mixed ? fminf(1.f, h.tau) : h.tau);
+    // kernel makes of it is overwritten when its block is done again).  Below -kFar: the reference was 0, those logits not being finite.  A row of a weight below 2^-40 has no room for a
+    // sum of exp(40) in its scale: it takes its maximum too.
+    const int i = h.i0 + b0 + r, t = h.rows[i];
+    const float weight = h.weight ? h.weight[t] : 1.0f / (float)*h.count;
+    const float span = far * 0.693147181f, most_span = h.e && fabsf(weight) < 0x1p-40f ? 1.f : kFar;
+    if (!OWN && !h.again && fabsf(span) > most_span && fabsf(far) < 1e30f && lane == 0) {
+      h.ref[i] += span * (h.mixed ? fminf(1.f, h.tau) : h.tau);
       h.redo[0] = 1;
       h.redo[1 + b0 / 256] = 1;
     }
-    const int i = h.i0 + b0 + r, t = h.rows[i];
     const bool hard = h.flags ? h.flags[t] & ROW_HARD : true, soft = h.flags ? h.flags[t] & ROW_SOFT : false;
     const float ref = OWN ? (far == -INFINITY ? 0.f : far) : h.ref[i], it = 1.0f / h.tau;
     const float* zs = h.zsel + (size_t)i * (h.top + 1);
@@ -763,9 +765,10 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
       if (h.row_lse) h.row_lse[t] = ref * it + logf(st);
     }
     if (!h.e) return;
-    const float g = h.weight ? h.weight[t] : 1.0f / (float)*h.count;
-    const float c1 = hard ? g * (1.f - h.share) : 0.f, ct = soft ? g * h.share * h.tau : 0.f;
-    const float p1 = c1 / sa, pt = ct / st, C = p1 + pt;          // dz = p1 e1 + pt et - sub
+    // dz = g (p1 e1 + pt et - sub).  The larger coefficient goes into g: 1 / C stays finite whatever the row's weight and share, and g is in the row's scale alone.
+    const float k1 = hard ? 1.f - h.share : 0.f, kt = soft ? h.share * h.tau : 0.f, most = fmaxf(fmaxf(k1, kt), 1e-37f);
+    const float g = weight * most, c1 = k1 / most, ct = kt / most;
+    const float p1 = c1 / sa, pt = ct / st, C = p1 + pt;
     const float inv = C != 0.f ? 1.0f / C : 0.f;
     if (h.coef && lane == 0) h.coef[b0 + r] = make_float2(p1 * inv, pt * inv);
     if (!h.places) return;
@@ -808,14 +811,14 @@ __global__ __launch_bounds__(1024) void head_fin_kernel(HeadFin h) {
       }
     }
     if (hard && !__ballot(y_listed) && lane == 0) { at[2] = y; val[2] = place(zy, c1); }
-    // The row of dz is C e.  Most of its length lies in the largest place (at the target p - 1 against many small p), so C is moved by the at most 2^-8 that make that place's rounded
+    // The row of dz is g C e.  Most of its length lies in the largest place (at the target p - 1 against many small p), so C is moved by the at most 2^-8 that make that place's rounded
     // value exact, and the rounding error of the whole gradient is that of its smaller part (128 x 2048, vocab 32000: dX 2.4e-3 -> 1.8e-3 from the exact values, 1.7e-3 of it its own
     // rounding).
     float big = fmaxf(fmaxf(fabsf(val[0]), fabsf(val[1])), fabsf(val[2]));
     big = wave_max(big);
     const float rounded = bf16_to_f32(f32_to_bf16(big));
     const float move = big > 0.f && big < 1e37f ? rounded / big : 1.f;          // exact e -> stored e
-    if (lane == 0) h.scale[i] = C / move;
+    if (lane == 0) h.scale[i] = g * (C / move);
     bf16_t* e = h.e + (size_t)(b0 + r) * h.vp;
 #pragma unroll
     for (int k = 0; k < 3; ++k)

@@ -35,3 +35,31 @@ def test_rows_whose_first_entries_are_absent(n, vocab, top, gone, dtype, tau, sh
     a = dict(ids=ids, u=u, tau=tau, share=share)
     strict(call(x, w, y, dw=(0, vocab), **a), x, w, y, dw=(0, vocab), **a)
     strict(call(x, w, y, dx=False, **a), x, w, y, **a)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [9, 333])
+@pytest.mark.parametrize("top,tau,share", [(0, 1.0, 1.0), (4, 1.0, 0.5), (4, 2.0, 1.0), (4, 3.0, 0.4)])
+def test_weights_down_to_the_smallest_floats(top, tau, share, n, dtype):
+    """Weights that fade along a sequence, down to numbers below the smallest normal float, and up to 1e20: rows of them have their part of the gradients or none, and spoil nothing."""
+    print(f"case head fading weights n={n} top={top} tau={tau} share={share} {dtype}", flush=True)
+    x, w, y, ids, u = make(n, 900, 64, TYPES[dtype], top=top, seed=8, ignored=0.1, ragged=False)
+    weight = 10.0 ** torch.linspace(0.0, -44.0, n, dtype=torch.float64, device="cuda")
+    weight[::3] *= -1
+    weight = weight.float()
+    # some rows' largest logit 39 above the target's
+    w[:, 0] = 0.0
+    w[7, 0], w[11, 0] = 1.0, -1.0
+    x[:, 0] = 0.0
+    x[3::5, 0], y[3::5] = 19.5, 11
+    if top:
+        ids[3::5, 0] = 11
+    a = dict(ids=ids, u=u, tau=tau, share=share) if top else {}
+    for scale in (1.0, 1e20):
+        wt = (weight * scale).contiguous()
+        strict(call(x, w, y, weight=wt, dw=(0, 900), dw_type=torch.float32, **a), x, w, y, weight=wt, dw=(0, 900), **a)
+    # nothing but small weights, a power of two: the gradients are those of weights of 1 times it, bit for bit
+    small = 2.0 ** -40
+    got, one = (call(x, w, y, weight=torch.full((n,), v, device="cuda"), dw=(0, 900), dw_type=torch.float32, **a) for v in (small, 1.0))
+    for name in ("dx", "dw"):
+        assert np.array_equal(got[name], small * one[name]), name
