@@ -25,6 +25,9 @@
 #include <atomic>
 #include <mutex>
 
+// m0 on the clobber lists below is reserved, hence not preserved, which is what the lists say
+#pragma clang diagnostic ignored "-Winline-asm"
+
 namespace pp {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -305,15 +308,15 @@ __global__ __launch_bounds__(512) void gemm_nt_mfma_dl_kernel(const bf16_t* __re
   // BK_FIRST: the same loads in assembly (they write no registers): the compiler, which would wait for every load into LDS that it knows of in front of a transpose read, knows of none
   const uint32_t lds0 = (uint32_t)(uintptr_t)PP_LPTR(lds);
   auto load_lds = [&](uint32_t dst, uint32_t off, const char* base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(dst)), "v"(off), "s"(base) : "m0", "memory");
   };
-  // the same in assembly for kernels whose main loop loads by the builtin (every load of either kind sets m0 for itself)
+  // the same in assembly for kernels whose main loop loads by the builtin (every load of either kind sets m0 for itself; the clobber keeps the compiler from expecting its own value there)
   [[maybe_unused]] auto issue_quiet = [&](const bf16_t* const (&g)[4], int s, int slot) {
     const size_t koff = (size_t)max(min(s, ns - 1), 0) * DL_BK;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds0 + (slot * DL_UNIT_CHUNKS + wdst + i * 64) * 16)), "v"(g[i] + koff)
-                   : "memory");
+                   : "m0", "memory");
   };
   auto issueA = [&](int s, int slot) {
     if constexpr (BK_FIRST) {
