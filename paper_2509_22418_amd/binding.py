@@ -388,11 +388,16 @@ class LocalStepModel:
         return self.loss
 
     def step_distill(self, tokens_dev, targets_dev, ids_dev, logits_dev, temperature: float, share: float, hp: dict | None):
-        """step() with the distillation loss (a model with head_pieces): ids_dev int32 and logits_dev float32 [B, S, top]; targets_dev may be None if share == 1."""
-        B, S, top = ids_dev.shape
+        """step() with the distillation loss (a model with head_pieces): ids_dev int32 and logits_dev float32 [B, S, top], tokens_dev and targets_dev int32 [B, S], all of them contiguous and on
+        the model's device; targets_dev may be None, and is not looked at, if share == 1."""
         t = self.torch
-        if tuple(tokens_dev.shape) != (B, S) or tuple(logits_dev.shape) != (B, S, top) or ids_dev.dtype != t.int32 or logits_dev.dtype != t.float32 or not ids_dev.is_contiguous() or not logits_dev.is_contiguous():
-            raise PPError("step_distill: ids must be contiguous int32 and logits contiguous float32, both [B, S, top]")
+        if ids_dev.dim() != 3:
+            raise PPError(f"step_distill: ids must be [B, S, top], not {tuple(ids_dev.shape)}")
+        B, S, top = ids_dev.shape
+        for name, x, shape, dtype in (("tokens", tokens_dev, (B, S), t.int32), ("targets", None if share == 1 else targets_dev, (B, S), t.int32), ("ids", ids_dev, (B, S, top), t.int32),
+                                      ("logits", logits_dev, (B, S, top), t.float32)):
+            if x is not None and (tuple(x.shape) != shape or x.dtype != dtype or x.device != self.loss.device or not x.is_contiguous()):
+                raise PPError(f"step_distill: {name} must be contiguous {dtype} {shape} on {self.loss.device}")
         opt = None if hp is None else PPAdamW(hp["lr"], hp["beta1"], hp["beta2"], hp["eps"], hp["weight_decay"])
         pp_local_step_distill(self.h, tokens_dev.data_ptr(), None if targets_dev is None else targets_dev.data_ptr(), B, S, ids_dev.data_ptr(), logits_dev.data_ptr(), top, temperature, share,
                               opt, self.loss.data_ptr())
