@@ -85,8 +85,9 @@ typedef struct {
   const void *x, *w;               /* storage type dtype */
   const float* row_weight;         /* [n] or NULL */
   float* loss;                     /* [1] or NULL */
-  float *row_loss, *row_lse;       /* [n] or NULL: l_t; log-sum-exp of z_t / temperature (pp_op_head_ce and share 0: of z_t) */
-  void *dx, *dw;                   /* dx [n x d], storage type, or NULL; dw [(dw_hi - dw_lo) x d], or NULL if dw_lo == dw_hi.  Neither may overlap an input. */
+  float *row_loss, *row_lse;       /* [n] or NULL: l_t; log-sum-exp of z_t / temperature (pp_op_head_ce and share 0: of z_t).  None of the three may overlap an input. */
+  void *dx, *dw;                   /* dx [n x d], storage type, or NULL; dw [(dw_hi - dw_lo) x d], or NULL if dw_lo == dw_hi.  Neither may
+                                      overlap another operand (column ranges of one buffer do not). */
   int32_t ldx, ldw, lddx, lddw;    /* elements from row to row, >= d (lddx, lddw: where dx, dw are given) */
   int32_t dtype, n, vocab, d;      /* PP_F32 or PP_BF16; n <= 2^24, vocab <= 2^20, d <= 2^14 */
   int32_t dw_lo, dw_hi;            /* 0 <= dw_lo <= dw_hi <= vocab; row 0 of dw is row dw_lo of W */
@@ -96,7 +97,8 @@ typedef struct {
 } pp_head;
 /* Workspace of a call with these sizes, options and operand alignment (top: entries per row, 0 for pp_op_head_ce); 0 and an error text on invalid arguments. */
 size_t pp_op_head_bytes(const pp_head* head, int32_t top);
-/* targets_dev: int32 [n].  ws_dev: 256-byte aligned, ws_bytes >= pp_op_head_bytes; the content does not matter and is not kept.  Calls that overlap need a workspace each. */
+/* targets_dev: int32 [n].  ws_dev: 256-byte aligned, ws_bytes >= pp_op_head_bytes; it may overlap no operand; the content does not matter and is not kept.
+ * Calls that overlap in time need a workspace each. */
 int pp_op_head_ce(void* hip_stream, const pp_head* head, const int32_t* targets_dev, void* ws_dev, size_t ws_bytes);
 /* ids_dev: int32 [n x top], logits_dev: float [n x top], 1 <= top <= PP_HEAD_TOP_MAX; temperature in [2^-6, 2^6]; share in [0, 1]; targets_dev may be NULL if share == 1. */
 int pp_op_head_distill(void* hip_stream, const pp_head* head, const int32_t* ids_dev, const float* logits_dev, int32_t top, float temperature, float share,

@@ -1138,10 +1138,52 @@ static int check_head(const pp_head* h, int top, HeadArgs* a) {
                 h->dw_lo, h->dw_hi, h->dw_f32, h->piece, nullptr, nullptr, nullptr, top, 1.f, 0.f, nullptr, 0, 0, 0};
   return PP_OK;
 }
+// Whether rows of a meet rows of b: rows of `width` bytes, `pitch` >= width bytes apart.  Exact, since column ranges of one buffer are separate operands.
+namespace pp {
+bool rows_overlap(const void* a, size_t width_a, size_t pitch_a, size_t rows_a, const void* b, size_t width_b, size_t pitch_b, size_t rows_b) {
+  if (!a || !b || !width_a || !width_b || !rows_a || !rows_b) return false;
+  if (rows_a > rows_b) return rows_overlap(b, width_b, pitch_b, rows_b, a, width_a, pitch_a, rows_a);
+  const int64_t pa = (int64_t)pitch_a, pb = (int64_t)pitch_b, wa = (int64_t)width_a, wb = (int64_t)width_b, na = (int64_t)rows_a, nb = (int64_t)rows_b;
+  const int64_t off = (int64_t)((uintptr_t)b - (uintptr_t)a);          // b's first byte, counted from a's
+  if (off >= (na - 1) * pa + wa || off + (nb - 1) * pb + wb <= 0) return false;
+  auto meets = [&](int64_t i) {          // the last row of b that starts in front of the end of a's row i
+    const int64_t end = i * pa + wa;
+    if (off >= end) return false;
+    const int64_t j = std::min(nb - 1, (end - 1 - off) / pb);
+    return off + j * pb + wb > i * pa;
+  };
+  const int64_t first = off > 0 ? std::max<int64_t>(0, (off - wa) / pa) : 0;          // rows of a in front of b's begin have nothing to meet
+  const int64_t last = std::min(na - 1, (off + (nb - 1) * pb + wb - 1) / pa);
+  if (pa == pb)          // the same columns of b along its rows: the first row and the last one have all there is
+    return first <= last && (meets(first) || meets(std::min(first + 1, last)) || meets(last));
+  for (int64_t i = first; i <= last; ++i)
+    if (meets(i)) return true;
+  return false;
+}
+}  // namespace pp
+// What is written (the gradients, the row outputs, the workspace) must not share a byte with what is read, nor the gradients and the workspace with anything.
+static int check_head_places(const char* who, const HeadArgs& a, const void* ws) {
+  struct Place { const char* name; const void* p; size_t width, pitch, rows; };
+  const size_t es = a.dtype == PP_F32 ? 4 : 2, gs = a.dw_f32 ? 4 : es, n = (size_t)a.n;
+  auto flat = [](const char* name, const void* p, size_t bytes) { return Place{name, p, bytes, bytes, 1}; };
+  const Place read[] = {{"x", a.x, a.d * es, a.ldx * es, n}, {"w", a.w, a.d * es, a.ldw * es, (size_t)a.vocab}, flat("row_weight", a.row_weight, n * 4), flat("targets", a.targets, n * 4),
+                        flat("ids", a.ids, n * a.top * 4), flat("logits", a.logits, n * a.top * 4)};
+  const Place wrote[] = {{"dx", a.dx, a.d * es, a.lddx * es, n}, {"dw", a.dw, a.d * gs, a.lddw * gs, (size_t)(a.dw_hi - a.dw_lo)}, flat("workspace", ws, head_bytes(a)),
+                         flat("loss", a.loss, 4), flat("row_loss", a.row_loss, n * 4), flat("row_lse", a.row_lse, n * 4)};
+  auto clash = [&](const Place& p, const Place& q) { return rows_overlap(p.p, p.width, p.pitch, p.rows, q.p, q.width, q.pitch, q.rows); };
+  auto refuse = [&](const Place& p, const Place& q) { return fail(PP_EINVAL, std::string(who) + ": " + p.name + " is in the place of another operand (" + q.name + ")"); };
+  for (const Place& p : wrote) {
+    for (const Place& q : read)
+      if (clash(p, q)) return refuse(p, q);
+    for (const Place* q = wrote; q < wrote + 3 && q != &p; ++q)
+      if (clash(p, *q)) return refuse(p, *q);
+  }
+  return PP_OK;
+}
 static int run_head(const char* who, void* hip_stream, const HeadArgs& a, void* ws, size_t ws_bytes) {
   if (!ws || ((uintptr_t)ws & 255)) return fail(PP_EINVAL, std::string(who) + ": workspace is NULL or not 256-byte aligned");
   if (ws_bytes < head_bytes(a)) return fail(PP_EINVAL, std::string(who) + ": workspace of " + std::to_string(ws_bytes) + " bytes, needs " + std::to_string(head_bytes(a)) + " (pp_op_head_bytes)");
-  if ((a.dx && (a.dx == a.x || a.dx == a.w)) || (a.dw && (a.dw == a.x || a.dw == a.w || a.dw == a.dx))) return fail(PP_EINVAL, std::string(who) + ": dx or dw is in the place of another operand");
+  if (int rc = check_head_places(who, a, ws)) return rc;
   int dev = 0;
   hipDevice_t own = 0;
   if (hip_stream) {

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2509_22418_amd as pp
 from test_gpu_head import TYPES, call, check, make
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +64,18 @@ def test_weights_down_to_the_smallest_floats(top, tau, share, n, dtype):
     got, one = (call(x, w, y, weight=torch.full((n,), v, device="cuda"), dw=(0, 900), dw_type=torch.float32, **a) for v in (small, 1.0))
     for name in ("dx", "dw"):
         assert np.array_equal(got[name], small * one[name]), name
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [7, 200])
+def test_operands_side_by_side_in_one_buffer(n, dtype):
+    """X and dX, W and dW as column ranges of one buffer each: they share no element, and the call is as with buffers of their own."""
+    x, w, y, _, _ = make(n, 500, 72, TYPES[dtype])
+    one, two = torch.zeros((n, 144), dtype=x.dtype, device="cuda"), torch.zeros((500, 200), dtype=x.dtype, device="cuda")
+    one[:, :72], two[:, 100:172] = x, w
+    out = dict(loss=torch.empty(1, device="cuda"), row_loss=torch.empty(n, device="cuda"), row_lse=torch.empty(n, device="cuda"), dx=one[:, 72:], dw=two[20:420, :72])
+    h = pp.make_head(one[:, :72], two[:, 100:172], dw_lo=5, dw_hi=405, **out)
+    ws = torch.empty(pp.pp_op_head_bytes(h), dtype=torch.uint8, device="cuda")
+    pp.pp_op_head_ce(torch.cuda.current_stream().cuda_stream, h, y.data_ptr(), ws.data_ptr(), ws.numel())
+    strict({k: v.double().cpu().numpy() for k, v in out.items()}, x, w, y, dw=(5, 405))
+    assert torch.equal(one[:, :72], x) and torch.equal(two[:, 100:172], w) and not two[420:, :72].any() and not two[:20, :72].any()

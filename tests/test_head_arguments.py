@@ -1,4 +1,7 @@
 """Arguments of the output head's losses that the binding and the library refuse, and calls next to those that they take.  No GPU: nothing is launched."""
+import ctypes
+import random
+
 import pytest
 import torch
 
@@ -40,3 +43,64 @@ def test_distilled_step_refuses_tensors_of_another_device(name):
     a[name + "_dev"] = a[name + "_dev"].to("meta")
     with pytest.raises(pp.PPError, match=f"step_distill: {name}"):
         holder().step_distill(**a)
+
+
+# ------------------------------------------------------------------------------------------------ operands in each other's place
+def rows_overlap(*a):
+    f = pp.load_library()["_ZN2pp12rows_overlapEPKvmmmS1_mmm"]
+    f.restype, f.argtypes = ctypes.c_bool, 2 * [ctypes.c_void_p, ctypes.c_size_t, ctypes.c_size_t, ctypes.c_size_t]
+    return f(*a)
+
+
+def test_overlap_of_rows_is_exact():
+    """Against sets of bytes: rows of all pitches, equal ones (column ranges of one buffer) among them, none and one row."""
+    r = random.Random(0)
+    seen = [0, 0]
+    for k in range(6000):
+        a, b = ([r.randint(1, 80), r.randint(0, 6), 0, r.randint(0, 7)] for _ in range(2))
+        for v in (a, b):
+            v[2] = v[1] + r.randint(0, 9)
+        if k % 2:          # one buffer
+            a[2] = b[2] = max(a[2], b[2])
+        p, q = ({v[0] + i * v[2] + c for i in range(v[3]) for c in range(v[1])} for v in (a, b))
+        assert rows_overlap(*a, *b) == bool(p & q), (a, b)
+        seen[bool(p & q)] += 1
+    assert min(seen) > 1000
+    big = 1 << 40          # 2^24 rows of 2^31 elements
+    assert not rows_overlap(big, 64, 1 << 33, 1 << 24, big + 64, 64, 1 << 33, 1 << 24)
+    assert rows_overlap(big, 65, 1 << 33, 1 << 24, big + 64, 64, 1 << 33, 1 << 24)
+
+
+M = 1 << 20
+PLACES = dict(x=1 * M, w=2 * M, row_weight=3 * M, loss=4 * M, row_loss=5 * M, row_lse=6 * M, dx=7 * M, dw=8 * M)
+SIZES = dict(x=10 * 128, w=100 * 128, row_weight=40, loss=4, row_loss=40, row_lse=40, dx=10 * 128, dw=100 * 128)
+CALL = dict(targets=9 * M, ids=10 * M, logits=11 * M)
+ROWS = [("dx", "x"), ("dx", "w"), ("dx", "row_weight"), ("dx", "targets"), ("dx", "ids"), ("dx", "logits"), ("dx", "dw"), ("dx", "row_loss"), ("dx", "row_lse"), ("dx", "loss"), ("dw", "x"), ("dw", "w"),
+        ("dw", "row_weight"), ("dw", "targets"), ("dw", "logits"), ("dw", "row_lse"), ("row_loss", "row_weight"), ("row_loss", "targets"), ("row_lse", "logits"), ("row_lse", "x"), ("loss", "ids"),
+        ("loss", "row_weight")] + [("workspace", k) for k in ("x", "w", "row_weight", "loss", "row_loss", "row_lse", "dx", "dw", "targets", "ids", "logits")]
+
+
+@pytest.mark.parametrize("first,second", ROWS)
+def test_operands_that_share_bytes_are_refused(first, second):
+    """The first operand's last four bytes on the second's first ones, and the other way around."""
+    for swap in (False, True):
+        at = dict(PLACES, **CALL, workspace=16 * M)
+        size = dict(SIZES, targets=40, ids=160, logits=160)
+        if first == "workspace":          # aligned: it begins 256 bytes behind the beginning of a large operand, or it holds the other
+            at[second] = at["workspace"] - (256 if swap and size[second] > 256 else -512)
+        elif swap:
+            at[first] = at[second] + size[second] - 4
+        else:
+            at[first] = at[second] - size[first] + 4
+        h = pp.PPHead(*[at[k] for k in ("x", "w", "row_weight", "loss", "row_loss", "row_lse", "dx", "dw")], 64, 64, 64, 64, pp.PP_BF16, 10, 100, 64, 0, 100, 0, 0)
+        with pytest.raises(pp.PPError, match="place of another operand") as e:
+            pp.pp_op_head_distill(None, h, at["ids"], at["logits"], 4, 1.0, 0.5, at["targets"], at["workspace"], 1 << 40)
+        assert first in str(e.value) and second in str(e.value)
+
+
+@pytest.mark.parametrize("over", [dict(dx=M + 128), dict(dx=M + 64 * 128 // 2 + 1200), dict(dw=2 * M - 128), dict(dw=2 * M + 128 * 50)])
+def test_gradients_that_begin_inside_an_operand_are_refused(over):
+    at = dict(PLACES, **over)
+    h = pp.PPHead(*[at[k] for k in ("x", "w", "row_weight", "loss", "row_loss", "row_lse", "dx", "dw")], 128, 64, 64, 64, pp.PP_BF16, 40, 100, 64, 0, 100, 0, 0)
+    with pytest.raises(pp.PPError, match="place of another operand"):
+        pp.pp_op_head_ce(None, h, 9 * M, 16 * M, 1 << 40)
