@@ -110,6 +110,13 @@ static HeadArgs step_head(const pp_config& c, bool dw, bool dx, int n) {
   return a;
 }
 
+// What the head's losses take in the step's workspace; no less for more rows, more entries or more gradients, so that one plan serves every batch
+static size_t head_in_step(const pp_config& c, bool dw, bool dx, int n, int top) {
+  HeadArgs a = step_head(c, dw, dx, n);
+  a.top = top;
+  return head_bytes(a);
+}
+
 static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
   WsPlan p{};
   const size_t es = esize(c), d = c.d_model, F = c.d_ff, V = c.vocab, h = c.n_heads, dh = d / h;
@@ -161,9 +168,7 @@ static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
   p.partial_bytes = any_dw ? kPartialCap : 0;
   p.partial = take(p.partial_bytes);
   if (p.pieces) {
-    HeadArgs a = step_head(c, m.lm, true, (int)T);
-    a.top = PP_HEAD_TOP_MAX;
-    p.head_bytes = head_bytes(a);
+    p.head_bytes = head_in_step(c, m.lm, true, (int)T, PP_HEAD_TOP_MAX);
     p.head = take(p.head_bytes);
   }
   p.total = off;
@@ -171,6 +176,9 @@ static WsPlan plan_ws(const pp_config& c, const Mask* mk) {
 }
 
 }  // namespace
+namespace pp {
+size_t step_head_bytes(const pp_config& c, bool dw, bool dx, int n, int top) { return head_in_step(c, dw, dx, n, top); }          // for tests of the plan
+}
 
 struct pp_model {
   pp_config cfg;
@@ -713,6 +721,25 @@ static int local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* tar
   };
   auto ofs = [&](void* p, size_t elems) { return (void*)((char*)p + elems * es); };
 
+  const bool any_layer = mk.norms || mk.heads || mk.wo || mk.ffn;
+  void* nf = W + w.nf;
+  void* dn = W + w.dn;
+  float* g = m->sg;
+  HeadArgs head{};
+  if (w.pieces) {
+    head = step_head(c, mk.lm, any_layer || mk.emb, T);
+    head.x = nf; head.w = canon(ly.lm_head); head.wt = shad(ly.sh_lm_head);
+    head.loss = loss_dev; head.row_loss = (float*)(W + w.rowloss);
+    if (head.dx) head.dx = dn;
+    if (head.dw) head.dw = g + find_seg(m, TK_LM_HEAD, -1)->packed_off;
+    head.targets = targets_dev;
+    if (kd) { head.ids = kd->ids; head.logits = kd->logits; head.top = kd->top; head.tau = kd->share > 0.f ? kd->tau : 1.f; head.share = kd->share; if (kd->share == 1.f) head.targets = nullptr; }
+    HeadArgs few = head;
+    few.no_few = 0; few.part_cap = 0;
+    if (head_is_few(few) && head_bytes(few) <= w.head_bytes) head = few;
+    if (head_bytes(head) > w.head_bytes) return fail(PP_EINVAL, "pp_local_step: the losses of the head need more workspace for this batch than was planned for the largest");
+  }
+
   // ---------------- forward over all parameters (Section 2.2: "the forward pass is standard")
   m->flops_fwd = 0; m->flops_bwd = 0; m->flops_recompute = 0;
   m->n_mfma = 0; m->n_plain = 0;
@@ -738,30 +765,16 @@ static int local_step(pp_model* m, const int32_t* tokens_dev, const int32_t* tar
   };
   for (int l = 0; l < L; ++l) layer_forward(l, (l + 1 < L) ? act(l + 1, w.a_x) : (void*)(W + w.xL));
   void* xL = W + w.xL;
-  void* nf = W + w.nf;
   void* logits = W + w.logits;
   float* rstdf = (float*)(W + w.rstdf);
   k_rmsnorm_fwd(st, dt, xL, canon(ly.final_norm), nf, rstdf, T, d, c.rms_eps);
-  const bool any_layer = mk.norms || mk.heads || mk.wo || mk.ffn;
-  void* dn = W + w.dn;
-  float* g = m->sg;
   if (w.pieces) {          // losses and gradients of the head, its logits a piece at a time
-    HeadArgs h = step_head(c, mk.lm, any_layer || mk.emb, T);
-    h.x = nf; h.w = canon(ly.lm_head); h.wt = shad(ly.sh_lm_head);
-    h.loss = loss_dev; h.row_loss = (float*)(W + w.rowloss);
-    if (h.dx) h.dx = dn;
-    if (h.dw) h.dw = g + find_seg(m, TK_LM_HEAD, -1)->packed_off;
-    h.targets = targets_dev;
-    if (kd) { h.ids = kd->ids; h.logits = kd->logits; h.top = kd->top; h.tau = kd->share > 0.f ? kd->tau : 1.f; h.share = kd->share; if (kd->share == 1.f) h.targets = nullptr; }
-    HeadArgs few = h;
-    few.no_few = 0; few.part_cap = 0;
-    if (head_is_few(few) && head_bytes(few) <= w.head_bytes) h = few;
-    if (k_head(st, h, W + w.head) != 0) return fail(PP_EHIP, "pp_local_step: a kernel of the head could not be set up on this device");
+    if (k_head(st, head, W + w.head) != 0) return fail(PP_EHIP, "pp_local_step: a kernel of the head could not be set up on this device");
     const double product = 2.0 * T * (double)V * d;
-    const int grads = (h.dx ? 1 : 0) + (h.dw ? 1 : 0);
+    const int grads = (head.dx ? 1 : 0) + (head.dw ? 1 : 0);
     m->flops_fwd += product; m->flops_bwd += product * grads;
     if (dt == PP_F32) m->n_plain += 1 + grads;
-    else if (head_is_few(h)) { m->n_mfma += 1; m->n_plain += grads; }
+    else if (head_is_few(head)) { m->n_mfma += 1; m->n_plain += grads; }
     else m->n_mfma += 1 + grads;
   } else {
     gemm_nt(m, nf, d, canon(ly.lm_head), d, logits, V, T, V, d);

@@ -104,3 +104,22 @@ def test_gradients_that_begin_inside_an_operand_are_refused(over):
     h = pp.PPHead(*[at[k] for k in ("x", "w", "row_weight", "loss", "row_loss", "row_lse", "dx", "dw")], 128, 64, 64, 64, pp.PP_BF16, 40, 100, 64, 0, 100, 0, 0)
     with pytest.raises(pp.PPError, match="place of another operand"):
         pp.pp_op_head_ce(None, h, 9 * M, 16 * M, 1 << 40)
+
+
+# ------------------------------------------------------------------------------------------------ the step's workspace
+def test_no_batch_needs_more_workspace_than_the_largest():
+    """A model plans its head's workspace once, for max_batch x max_seq tokens and the longest lists: every smaller batch, list and set of gradients has to fit."""
+    f = pp.load_library()["_ZN2pp15step_head_bytesERK9pp_configbbii"]
+    f.restype, f.argtypes = ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_bool, ctypes.c_bool, ctypes.c_int, ctypes.c_int]
+    r = random.Random(1)
+    for dtype in (pp.PP_F32, pp.PP_BF16):
+        for vocab, d, most in [(8, 8, 40000), (512, 128, 1 << 18), (8000, 512, 9000), (20000, 64, 5000), (32000, 768, 16384), (32000, 2048, 16384), (50264, 776, 5000), (128000, 4096, 8192), (1 << 20, 1 << 14, 4096),
+                               (1 << 20, 64, 1 << 15)] + [(8 * r.randint(1, 20000), 8 * r.randint(1, 512), r.randint(1, 20000)) for _ in range(30)]:
+            c = pp.PPConfig(1, d, 1, 8, vocab, 1, most, dtype, 1e-5, 1e4, pp.PP_HEAD_PIECES)
+            for trained in (False, True):
+                planned = f(ctypes.byref(c), trained, True, most, pp.PP_HEAD_TOP_MAX)
+                sizes = {1, 16, 17, 64, 65, 256, 257, most, most - 1, *(int(most ** r.random()) for _ in range(20)), *(r.randint(1, most) for _ in range(20))}
+                for n in sizes:
+                    for dw, dx, top in ((trained, True, 0), (trained, False, 128), (trained, True, r.randint(1, 128)), (False, False, 0), (False, True, r.choice((1, 2, 8, 64, 128)))):
+                        if 0 < n <= most:
+                            assert f(ctypes.byref(c), dw, dx, n, top) <= planned, (dtype, vocab, d, most, trained, n, dw, dx, top)
