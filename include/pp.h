@@ -59,8 +59,11 @@ typedef struct {
                                  bit for bit; WORKSPACE shrinks by about (n_layers - 1) layers of activations.
                                  PP_HEAD_PIECES may be added to either (a bit): the output head's logits are not kept either.  Its loss and gradients
                                  are formed a piece of rows at a time (pp_op_head_ce in pp_ops.h states how, and the roundings; with bf16 storage the loss is
-                                 formed from fp32 logits, not from rounded ones), WORKSPACE holds about 0.4 GB and one copy of the final norm's output for them instead of B x S x vocab elements, and
-                                 vocab may be up to 2^20 (without: 65536 with bf16 storage, 16320 with fp32). */
+                                 formed from fp32 logits, not from rounded ones), and vocab may be up to 2^20 (without: 65536 with bf16 storage, 16320 with fp32).
+                                 Instead of B x S x vocab elements WORKSPACE holds a piece of logits (256 MiB at most, or 256 rows where those are larger), with bf16 storage
+                                 a fifth of that for the rows' sums and up to 1.1 KB a position for a teacher's lists, 64 MiB of partial sums, and a copy of the final norm's output (with bf16 and a
+                                 trainable lm_head one more of a piece of it).  Besides, with bf16 where d_model is no multiple of 64 a padded copy of lm_head, with fp32 where vocab is no
+                                 multiple of 128 a transposed one, and with fp32 where lm_head is trainable and the batch takes several pieces as much as its gradient, if that is more than the 64 MiB. */
 } pp_config;
 enum { PP_HEAD_PIECES = 4 };
 

@@ -123,3 +123,29 @@ def test_no_batch_needs_more_workspace_than_the_largest():
                     for dw, dx, top in ((trained, True, 0), (trained, False, 128), (trained, True, r.randint(1, 128)), (False, False, 0), (False, True, r.choice((1, 2, 8, 64, 128)))):
                         if 0 < n <= most:
                             assert f(ctypes.byref(c), dw, dx, n, top) <= planned, (dtype, vocab, d, most, trained, n, dw, dx, top)
+
+
+def stated(dtype, vocab, d, tokens, trained):
+    """What include/pp.h says PP_HEAD_PIECES holds, in bytes."""
+    up = lambda v, m: -(-v // m) * m  # noqa: E731
+    bf, es = dtype == pp.PP_BF16, 2 if dtype == pp.PP_BF16 else 4
+    rows = min(up(tokens, 64), max(256, (256 << 20) // (vocab * es) // 256 * 256))
+    logits = rows * up(vocab, 64 if bf else 128) * es
+    wide = up(d, 64 if bf else 4)
+    total = logits + (64 << 20) + up(tokens, 64) * wide * es
+    if bf:
+        return total + logits // 5 + 1100 * up(tokens, 64) + (rows * wide * es if trained else 0) + (vocab * wide * es if d % 64 else 0)
+    total += d * up(vocab, 128) * es if vocab % 128 else 0
+    return total + (max(0, vocab * d * es - (64 << 20)) if trained and rows < tokens else 0)
+
+
+@pytest.mark.parametrize("dtype", [pp.PP_F32, pp.PP_BF16])
+def test_the_head_takes_what_the_header_says(dtype):
+    f = pp.load_library()["_ZN2pp15step_head_bytesERK9pp_configbbii"]
+    f.restype, f.argtypes = ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_bool, ctypes.c_bool, ctypes.c_int, ctypes.c_int]
+    for vocab, d, tokens in [(512, 128, 192), (8000, 512, 9000), (20000, 64, 5000), (32000, 768, 16384), (32000, 2048, 16384), (50264, 776, 5000), (128000, 4096, 8192), (1 << 20, 64, 1 << 15),
+                             (1 << 20, 1 << 14, 4096), (1 << 20, 4096, 200), (40000, 1000, 1 << 17)]:
+        c = pp.PPConfig(1, d, 1, 8, vocab, 1, tokens, dtype, 1e-5, 1e4, pp.PP_HEAD_PIECES)
+        for trained in (False, True):
+            size, said = f(ctypes.byref(c), trained, True, tokens, pp.PP_HEAD_TOP_MAX), stated(dtype, vocab, d, tokens, trained)
+            assert said * 0.9 <= size <= said * 1.005 + (2 << 20), (vocab, d, tokens, trained, size >> 20, said >> 20)
