@@ -278,6 +278,10 @@ def make_head(x, w, *, row_weight=None, loss=None, row_loss=None, row_lse=None, 
         raise PPError("make_head: dw_add needs a float32 dw")
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     ld = lambda t: d if t is None or t.shape[0] < 2 else t.stride(0)  # noqa: E731
+    for name, v in (("rows of x", n), ("rows of w", vocab), ("columns", d), ("stride of x", ld(x)), ("stride of w", ld(w)), ("stride of dx", ld(dx)), ("stride of dw", ld(dw)), ("dw_lo", dw_lo), ("dw_hi", dw_hi),
+                    ("piece", piece)):
+        if not -1 << 31 <= v < 1 << 31:          # a C int would keep the lower half
+            raise PPError(f"make_head: {name}: {v} does not fit 32 bits")
     h = PPHead(ptr(x), ptr(w), ptr(row_weight), ptr(loss), ptr(row_loss), ptr(row_lse), ptr(dx), ptr(dw), ld(x), ld(w), ld(dx), ld(dw), PP_F32 if x.dtype == f32 else PP_BF16, n, vocab, d,
                dw_lo, dw_hi, 0 if dw is None else 2 if dw_add else 1 if dw.dtype == f32 else 0, piece)
     h.tensors = (x, w, row_weight, loss, row_loss, row_lse, dx, dw)

@@ -149,3 +149,22 @@ def test_the_head_takes_what_the_header_says(dtype):
         for trained in (False, True):
             size, said = f(ctypes.byref(c), trained, True, tokens, pp.PP_HEAD_TOP_MAX), stated(dtype, vocab, d, tokens, trained)
             assert said * 0.9 <= size <= said * 1.005 + (2 << 20), (vocab, d, tokens, trained, size >> 20, said >> 20)
+
+
+# ------------------------------------------------------------------------------------------------ make_head
+def meta(rows, cols, pitch=None):
+    return torch.empty_strided((rows, cols), (pitch or cols, 1), dtype=torch.bfloat16, device="meta")
+
+
+@pytest.mark.parametrize("x,w,over,text", [
+    (meta((1 << 32) + 5, 8), meta(20, 8), {}, "rows of x"), (meta(6, 8), meta((1 << 32) + 20, 8), {}, "rows of w"), (meta(6, 8, (1 << 32) + 8), meta(20, 8), {}, "stride of x"),
+    (meta(6, 8), meta(20, 8, 1 << 31), {}, "stride of w"), (meta(6, 8), meta(20, 8), dict(dx=meta(6, 8, 1 << 33)), "stride of dx"), (meta(6, 8), meta(20, 8), dict(dw=meta(20, 8, 1 << 33)), "stride of dw"),
+    (meta(6, 8), meta(20, 8), dict(piece=1 << 32), "piece"), (meta(6, 8), meta(20, 8), dict(dw_lo=1 << 32, dw_hi=(1 << 32) + 3, dw=meta(3, 8)), "dw_lo")])
+def test_sizes_beyond_32_bits_are_refused_and_not_cut(x, w, over, text):
+    with pytest.raises(pp.PPError, match=f"make_head: {text}"):
+        pp.make_head(x, w, **over)
+
+
+def test_largest_strides_are_taken():
+    h = pp.make_head(meta(6, 8, (1 << 31) - 1), meta(20, 8, (1 << 31) - 1))
+    assert (h.ldx, h.ldw) == ((1 << 31) - 1, (1 << 31) - 1)
