@@ -272,7 +272,7 @@ def make_head(x, w, *, row_weight=None, loss=None, row_loss=None, row_lse=None, 
             continue
         if tuple(t.shape) != shape or t.dtype not in types or t.device != x.device:
             raise PPError(f"make_head: {name} must be {shape} of {' or '.join(str(k) for k in types)} on {x.device}")
-        if t.numel() and t.stride(-1) != 1 or t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < d:
+        if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1 or t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < d:
             raise PPError(f"make_head: {name}: elements of a row must lie next to each other, rows one after the other")
     if dw_add and (dw is None or dw.dtype != f32):
         raise PPError("make_head: dw_add needs a float32 dw")

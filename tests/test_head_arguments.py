@@ -168,3 +168,12 @@ def test_sizes_beyond_32_bits_are_refused_and_not_cut(x, w, over, text):
 def test_largest_strides_are_taken():
     h = pp.make_head(meta(6, 8, (1 << 31) - 1), meta(20, 8, (1 << 31) - 1))
     assert (h.ldx, h.ldw) == ((1 << 31) - 1, (1 << 31) - 1)
+
+
+def test_single_columns_have_no_stride():
+    """The stride of a dimension of one element says nothing: a column of a wider tensor, one row weight, the column that a transposed row is."""
+    bf = torch.bfloat16
+    h = pp.make_head(torch.zeros((6, 8), dtype=bf)[:, 3:4], torch.zeros((1, 20), dtype=bf).t(), row_weight=torch.zeros(6))
+    assert (h.n, h.vocab, h.d, h.ldx, h.ldw) == (6, 20, 1, 8, 1)
+    h = pp.make_head(torch.zeros((1, 8), dtype=bf), torch.zeros((20, 8), dtype=bf), row_weight=torch.zeros(12)[::12], loss=torch.zeros(5)[::5])
+    assert (h.n, h.ldx) == (1, 8)
