@@ -78,8 +78,10 @@ int pp_op_attention_bwd(void* hip_stream, int dtype, const void* qkv_dev, const 
  * A row of weight 0 is left out too.  Rows that are left out have row_loss = row_lse = 0 and a dX row of zeros, and neither their values nor infinities or NaN among them reach
  * anything else.  n == 0 gives loss 0 and dW = 0.
  * Sums, exponentials and losses are fp32.  With bf16 storage and more than 16 rows, a row of dz enters the gradients' products as a multiple of a row that is rounded to
- * bf16 (at most 2^-8 relative, twice where both softmaxes count at a temperature other than 1), its multiple moved by at most 2^-8 so that the largest element is not rounded; the rows of X are
- * scaled by the multiple and rounded to bf16 for dW.  dX and dW are rounded once from fp32 sums.  Results do not depend on the run. */
+ * bf16 (at most 2^-8 relative), its multiple moved by at most 2^-8 so that the largest element is not rounded; the rows of X are scaled by the multiple and rounded to bf16 for dW.  Where both
+ * softmaxes count at a temperature other than 1 they are formed from the sharper one's exponent y (of two, against a reference no larger than the row's maximum), rounded to steps of 2^-8 down to
+ * y = -64 and of 2^-4 below, and taken as nothing below -2096: another 2^-9 ln 2, below -64 2^-5 ln 2, of the sharper part of an element and that over the ratio of the temperatures of the softer
+ * part.  Weights below 2^-100 in size may lose bits there.  dX and dW are rounded once from fp32 sums.  Results do not depend on the run. */
 #define PP_HEAD_TOP_MAX 128
 typedef struct {
   const void *x, *w;               /* storage type dtype */

@@ -79,3 +79,63 @@ def test_operands_side_by_side_in_one_buffer(n, dtype):
     pp.pp_op_head_ce(torch.cuda.current_stream().cuda_stream, h, y.data_ptr(), ws.data_ptr(), ws.numel())
     strict({k: v.double().cpu().numpy() for k, v in out.items()}, x, w, y, dw=(5, 405))
     assert torch.equal(one[:, :72], x) and torch.equal(two[:, 100:172], w) and not two[420:, :72].any() and not two[:20, :72].any()
+
+
+def tight(got, x, w, y, ids, u, tau, share, dw):
+    """strict(), and dX and dW of a call with more than 16 rows in bf16 within the sum of the roundings that the code makes, whatever the temperature.
+
+    An element of dz is a sum of the two softmaxes' parts and of what is taken off at the target and the entries.  Its roundings: an exponential's argument and sum in fp32 (`rel` each); the stored
+    sum of both parts to bf16 (half a step, 2^-8) and the row's scale, which moves by as much (2^-8).  Two softmaxes are formed from a stored exponent y of the sharper one, in powers of two: half
+    a step of it is 2^-9 from -64 on and 2^-5 below (of its largest logit, which no reference exceeds, so no y is larger than assumed here), hence 2^-9 ln 2 or 2^-5 ln 2 of the sharper part and
+    those over the ratio of the temperatures of the softer one; below -2096 both are taken as 0.  Then half a step for the scaled rows of X (dW), fp32 sums, and half a step of the results."""
+    ref = strict(got, x, w, y, ids, u, tau=tau, share=share, dw=dw)
+    X, W, Y, I = x.double().cpu().numpy(), w.double().cpu().numpy(), y.long().cpu().numpy(), ids.long().cpu().numpy()
+    n, vocab, d = X.shape[0], W.shape[0], X.shape[1]
+    live, eps, half, z = ref["live"], 2.0 ** -24, 2.0 ** -8, ref["z"]
+    X0 = np.where(live[:, None], X, 0.0)
+    g = np.where(live, 1.0 / max(1, live.sum()), 0.0)
+    it = max(1.0, 1.0 / tau)
+    there = (I >= 0) & (I < vocab) & (u.cpu().numpy() != -np.inf) & live[:, None]
+    c1 = g * (1 - share) * ((Y >= 0) & (Y < vocab))
+    ct = g * share * tau * there.any(1)
+    soft = lambda v: np.exp(v - v.max(1, keepdims=True)) / np.exp(v - v.max(1, keepdims=True)).sum(1, keepdims=True)  # noqa: E731
+    one, two = c1[:, None] * soft(z), ct[:, None] * soft(z / tau)
+    rel = ((d + 2) * eps * it * (np.abs(X0) @ np.abs(W).T)).max(1) + (2 * np.abs(z).max(1) * it + vocab / 64 + 80) * eps
+    off = np.zeros_like(z)
+    rows = np.broadcast_to(np.arange(n)[:, None], I.shape)
+    np.add.at(off, (rows[there], I[there]), (ct * np.ones(I.shape).T).T[there])
+    hard = np.nonzero(c1)[0]
+    off[hard, Y[hard]] += c1[hard]
+    err = np.abs(ref["dz"]) * (2 * rel[:, None] + 2 * half + 8 * eps) + off * (4 * rel[:, None] + 16 * eps)
+    if tau != 1.0 and 0.0 < share < 1.0:
+        ratio = max(tau, 1.0 / tau)
+        exponent = (z - z.max(1, keepdims=True)) * it / np.log(2.0)
+        step = np.where(exponent < -64, 2.0 ** -5, 2.0 ** -9) * np.log(2.0) * 1.02          # 2^s - 1 <= 1.02 s ln 2 for these s
+        sharper, softer = (one, two) if tau > 1.0 else (two, one)
+        lost = exponent < -2096
+        plain = off == 0          # places are formed in fp32
+        err += np.where(plain, sharper * np.where(lost, 1.0, step) + softer * np.where(lost, 1.0, step / ratio), 0.0)
+    part, absW, lo, hi = np.abs(ref["dz"]), np.abs(W), *dw
+    tol = err @ absW + (vocab + 64) * eps * (part @ absW) + half * np.abs(ref["dx"]) + 1e-36
+    worst = np.abs(got["dx"] - ref["dx"]) / tol
+    assert worst.max() <= 1, ("dx", float(worst.max()), np.argwhere(worst > 1)[:3].tolist())
+    tol = (err + part * half)[:, lo:hi].T @ np.abs(X0) + (n + 64) * eps * (part[:, lo:hi].T @ np.abs(X0)) + half * np.abs(ref["dw"][lo:hi]) + 1e-36
+    worst = np.abs(got["dw"] - ref["dw"][lo:hi]) / tol
+    assert worst.max() <= 1, ("dw", float(worst.max()), np.argwhere(worst > 1)[:3].tolist())
+
+
+@pytest.mark.parametrize("n,vocab", [(40, 600), (700, 3000), (2100, 4100)])
+@pytest.mark.parametrize("tau,std", [(64.0, 30.0), (16.0, 30.0), (3.0, 8.0), (2.0, 0.5), (1.5, 30.0), (0.7, 8.0), (0.7, 40.0), (0.5, 8.0), (0.25, 2.0), (0.125, 0.5), (0.125, 8.0), (1.0 / 64, 0.05), (1.0 / 64, 1.0),
+                                     (1.0 / 64, 5.0)])
+def test_two_softmaxes_within_their_roundings(tau, std, n, vocab):
+    print(f"case head two softmaxes {n}x{vocab} tau={tau} std={std}", flush=True)
+    x, w, y, ids, u = make(n, vocab, 64, torch.bfloat16, top=6, std=std, seed=4)
+    dw = (3, vocab - 2)
+    tight(call(x, w, y, ids, u, tau=tau, share=0.6, dw=dw), x, w, y, ids, u, tau, 0.6, dw)
+
+
+@pytest.mark.parametrize("tau,share", [(1.0, 1.0), (1.0, 0.4), (4.0, 1.0), (0.125, 1.0), (1.0 / 64, 1.0), (2.0, 0.0)])
+def test_one_softmax_within_its_roundings(tau, share):
+    x, w, y, ids, u = make(700, 3000, 64, torch.bfloat16, top=6, std=0.5, seed=4)
+    dw = (3, 2998)
+    tight(call(x, w, y, ids, u, tau=tau, share=share, dw=dw), x, w, y, ids, u, 1.0 if share == 0.0 else tau, share, dw)
