@@ -71,10 +71,13 @@ int pp_op_attention_bwd(void* hip_stream, int dtype, const void* qkv_dev, const 
  *   dX = dz W [n x d]   and   dW = dz^T X for the rows [dw_lo, dw_hi) of W
  * of   loss = sum_t w_t l_t,   w_t = row_weight[t], or 1 / (number of rows that are not left out) where row_weight is NULL (the mean, as in pp_local_step).
  *   pp_op_head_ce       l_t = lse(z_t) - z_t[target]; a row whose target is outside [0, vocab) is left out.
- *   pp_op_head_distill  l_t = (1 - share) CE_t + share temperature^2 KL(q_t || softmax(z_t / temperature)) with CE_t as above and
- *                       q_t = softmax(logits_t / temperature) over the `top` entries (id, logit) that the teacher lists for the row.  An id outside [0, vocab) or a logit of
- *                       -inf is no entry, whatever its other half holds; equal ids add up.  A row without entries has no KL term, a row without target no CE term, a row without
- *                       either (terms with a share of 0 do not count) is left out.
+ *   pp_op_head_distill  l_t = (1 - share) CE_t + share temperature^2 D_t with CE_t as above and, over the entries (id_j, logit_j) of the `top` that the teacher lists for the row,
+ *                         D_t = sum_j q_j (log q_j - log p[id_j]),   q = softmax(logits / temperature) over the entries,   p = softmax(z_t / temperature) over the vocabulary:
+ *                       KL(q || p) of a list of different ids.  An id that is listed more than once stands for the sum of its entries in the gradients, which are those of that divergence; in
+ *                       D_t each entry keeps its own logarithm, so that D_t is lower than the divergence by sum_j q_j log(Q_j / q_j), Q_j the sum of the entries with id_j (it does not depend on
+ *                       z, and D_t may be negative: merge the entries first where the value has to be a divergence).
+ *                       An id outside [0, vocab) or a logit of -inf is no entry, whatever its other half holds.  A row without entries has no D_t, a row without target no CE term, a row
+ *                       without either (terms with a share of 0 do not count) is left out.
  * A row of weight 0 is left out too.  Rows that are left out have row_loss = row_lse = 0 and a dX row of zeros, and neither their values nor infinities or NaN among them reach
  * anything else.  n == 0 gives loss 0 and dW = 0.
  * Sums, exponentials and losses are fp32.  With bf16 storage and more than 16 rows, a row of dz enters the gradients' products as a multiple of a row that is rounded to

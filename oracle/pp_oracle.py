@@ -576,8 +576,8 @@ def outer_step(theta_g, theta_l, others_sum, momentum_buf, lr, mu, m_count, nest
 
 
 def head_loss(x, w, targets, row_weight=None, ids=None, logits=None, tau=1.0, share=1.0):
-    """Losses of the output head from their definition, and their gradients: cross entropy where ids is None, else (1 - share) CE + share tau^2 KL(teacher || student) with the
-    teacher's softmax over its listed entries only.  Returns loss, row_loss, row_lse, z, dz, dx, dw (all rows of w) and live (rows that are not left out)."""
+    """Losses of the output head from their definition, and their gradients: cross entropy where ids is None, else (1 - share) CE + share tau^2 sum_j q_j (log q_j - log p[id_j]), q the
+    teacher's softmax over its listed entries only (KL(teacher || student) where no id is listed twice).  Returns loss, row_loss, row_lse, z, dz, dx, dw (all rows of w) and live (rows that are not left out)."""
     x, w = np.asarray(x, F64), np.asarray(w, F64)
     n, vocab = x.shape[0], w.shape[0]
     if ids is None:

@@ -139,3 +139,16 @@ def test_one_softmax_within_its_roundings(tau, share):
     x, w, y, ids, u = make(700, 3000, 64, torch.bfloat16, top=6, std=0.5, seed=4)
     dw = (3, 2998)
     tight(call(x, w, y, ids, u, tau=tau, share=share, dw=dw), x, w, y, ids, u, 1.0 if share == 0.0 else tau, share, dw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [5, 90])
+@pytest.mark.parametrize("tau,share", [(1.0, 1.0), (0.5, 1.0), (2.0, 0.5)])
+def test_lists_that_repeat_ids(tau, share, n, dtype):
+    """Rows of few words listed up to twelve times, their target among them: each entry keeps its own logarithm in the loss, and the gradients are those of the sums."""
+    x, w, y, ids, u = make(n, 400, 64, TYPES[dtype], top=20, ragged=False, seed=14)
+    ids = (ids % 5).int()
+    ids[::3, :12] = 7
+    y = torch.where(y >= 0, y % 8, y).int()
+    a = dict(ids=ids, u=u, tau=tau, share=share)
+    strict(call(x, w, y, dw=(0, 400), **a), x, w, y, dw=(0, 400), **a)
