@@ -249,11 +249,22 @@ def pp_op_head_bytes(head: PPHead, top: int = 0) -> int:
     return n
 
 
+def _check_head_device(head: PPHead, who: str):
+    """The calls launch on the current device; tensors that make_head knows to be on another one would be read there without a mapping."""
+    x = head.tensors[0] if getattr(head, "tensors", None) else None
+    if x is not None and x.is_cuda:
+        import torch
+        if x.device.index != torch.cuda.current_device():
+            raise PPError(f"{who}: the tensors are on {x.device}, and cuda:{torch.cuda.current_device()} is the current device")
+
+
 def pp_op_head_ce(stream: int, head: PPHead, targets_ptr, ws_ptr, ws_bytes: int):
+    _check_head_device(head, "pp_op_head_ce")
     _check(load_library().pp_op_head_ce(stream, C.byref(head), targets_ptr, ws_ptr, ws_bytes), "pp_op_head_ce")
 
 
 def pp_op_head_distill(stream: int, head: PPHead, ids_ptr, logits_ptr, top: int, temperature: float, share: float, targets_ptr, ws_ptr, ws_bytes: int):
+    _check_head_device(head, "pp_op_head_distill")
     _check(load_library().pp_op_head_distill(stream, C.byref(head), ids_ptr, logits_ptr, top, temperature, share, targets_ptr, ws_ptr, ws_bytes), "pp_op_head_distill")
 
 

@@ -1,6 +1,7 @@
 """Arguments of the output head's losses that the binding and the library refuse, and calls next to those that they take.  No GPU: nothing is launched."""
 import ctypes
 import random
+import types
 
 import pytest
 import torch
@@ -177,3 +178,15 @@ def test_single_columns_have_no_stride():
     assert (h.n, h.vocab, h.d, h.ldx, h.ldw) == (6, 20, 1, 8, 1)
     h = pp.make_head(torch.zeros((1, 8), dtype=bf), torch.zeros((20, 8), dtype=bf), row_weight=torch.zeros(12)[::12], loss=torch.zeros(5)[::5])
     assert (h.n, h.ldx) == (1, 8)
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    """With the default stream the library cannot tell: its kernels would run on the current device."""
+    h = pp.make_head(torch.zeros((6, 8)), torch.zeros((20, 8)))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    calls = (lambda: pp.pp_op_head_ce(None, h, 0x1000, None, 0), lambda: pp.pp_op_head_distill(None, h, 0x1000, 0x1000, 4, 1.0, 0.5, 0x1000, None, 0))
+    for index, text in ((1, "current device"), (0, "256-byte")):          # on the current one the call reaches the library, which refuses its missing workspace
+        h.tensors = (types.SimpleNamespace(is_cuda=True, device=torch.device("cuda", index)),)
+        for call in calls:
+            with pytest.raises(pp.PPError, match=text):
+                call()
