@@ -152,3 +152,19 @@ def test_lists_that_repeat_ids(tau, share, n, dtype):
     y = torch.where(y >= 0, y % 8, y).int()
     a = dict(ids=ids, u=u, tau=tau, share=share)
     strict(call(x, w, y, dw=(0, 400), **a), x, w, y, dw=(0, 400), **a)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [4, 16, 70])
+@pytest.mark.parametrize("top", [1, 3, 70, 128])
+def test_rows_of_nothing_but_minus_infinity(top, n, dtype):
+    """Valid ids whose logits are all -inf are no entries: such a row has no KL term, and is left out where it has no target either."""
+    x, w, y, ids, u = make(n, 300, 64, TYPES[dtype], top=top, ragged=False, seed=15, ignored=0.5)
+    u[::2] = -torch.inf
+    y[0], y[1] = -1, 5
+    x[0] = torch.nan
+    for tau, share in ((1.0, 1.0), (2.0, 0.5), (0.5, 0.25)):
+        a = dict(ids=ids, u=u, tau=tau, share=share)
+        got = call(x, w, y, dw=(0, 300), **a)
+        assert got["row_loss"][0] == 0 and not got["dx"][0].any()
+        strict(got, x, w, y, dw=(0, 300), **a)
